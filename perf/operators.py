@@ -227,15 +227,15 @@ def run(s):
 def _run_own(s):
     ctx, shape, op = s["ctx"], s["shape"], s["op"]
     if op == "decode_fp8":
-        return ctx.fkv_decode_attention_paged_fp8(shape, s["q"], s["k"], s["v"], s["k_scale"], s["v_scale"], s["table"], s["n"])
+        return ctx.fkv_decode_attention_paged_quant(shape, s["q"], s["k"], s["v"], s["k_scale"], s["v_scale"], s["table"], s["n"])
     if op == "gather_fp8":
-        ctx.fkv_gather_kv_paged_fp8(shape, s["k_new"], s["v_new"], s["idx"], s["budget"], s["table"], s["k"], s["v"], s["k_scale"], s["v_scale"])
+        ctx.fkv_gather_kv_paged_quant(shape, s["k_new"], s["v_new"], s["idx"], s["budget"], s["table"], s["k"], s["v"], s["k_scale"], s["v_scale"])
         return s["k"], s["v"], s["k_scale"], s["v_scale"]
     if op == "append":
         q = ctx.fkv_append_kv_paged(shape, s["k_new"], s["v_new"], s["n"], s["new"], s["table"], s["k"], s["v"], rope=s["rope"],
                                     positions=s["positions"], q=s["q"])
         return q, s["k"], s["v"]
-    q = ctx.fkv_append_kv_paged_fp8(shape, s["k_new"], s["v_new"], s["n"], s["new"], s["table"], s["k"], s["v"], s["k_scale"], s["v_scale"],
+    q = ctx.fkv_append_kv_paged_quant(shape, s["k_new"], s["v_new"], s["n"], s["new"], s["table"], s["k"], s["v"], s["k_scale"], s["v_scale"],
                                     rope=s["rope"], positions=s["positions"], q=s["q"])
     return q, s["k"], s["v"], s["k_scale"], s["v_scale"]
 
