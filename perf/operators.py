@@ -154,7 +154,7 @@ def _table(gen, counts, page):
 def _pow2_scale(a):
     """p(a): 448 is 0.875 * 2^9, so the power follows from the mantissa and exponent of a, exactly."""
     mant, exp = torch.frexp(a)
-    return torch.ldexp(torch.ones_like(a), exp - 9 + (mant > 0.875).to(exp.dtype)).clamp_min(TINY)
+    return torch.ldexp((a > 0).to(a.dtype), exp - 9 + (mant > 0.875).to(exp.dtype)).clamp_min(TINY)
 
 
 def _fp8_pool(gen, n_pages, hkv, page, block, std):
