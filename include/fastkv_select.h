@@ -254,6 +254,71 @@ int fkv_decode_attention_paged(fkv_ctx *ctx, const fkv_shape *shape, const void 
                                const void *v_pages, const int32_t *block_table, int32_t max_pages_per_seq,
                                int32_t page_size, int64_t n_pages, const int32_t *n_per_seq, float *out, void *stream);
 
+/* Rotary position embedding (host struct, read during the call only): columns x, y of pair i of a head's row become
+ * x cos(phi) - y sin(phi) and y cos(phi) + x sin(phi), phi = position * inv_freq[i].  The angle is reduced exactly (positions are
+ * whole numbers), sine and cosine are fp32 values within 2 ulp, and a result is rounded once to what it is stored as. */
+typedef struct fkv_rope {
+  int32_t rotary_dim;     /* r: the first r columns of a row take part, the others pass unchanged; a multiple of 16, 16 <= r <= d */
+  int32_t interleaved;    /* 0: columns i and i + r/2 are pair i; 1: columns 2i and 2i + 1 */
+  const double *inv_freq; /* host [r/2], radians per position, finite */
+} fkv_rope;
+
+/* The new tokens of a call that appends to a paged cache (host struct; n_new_b of sequence b, packed along tokens in that order). */
+typedef struct fkv_new_tokens {
+  const void *k, *v;        /* [sum n_new][Hkv][d] bf16, 16-byte aligned; a token's heads lie side by side */
+  const void *q;            /* [sum n_new][Hq][d] bf16: queries to be turned like the keys, or NULL */
+  void *q_out;              /* [sum n_new][Hq][d] bf16, given together with q; may be q itself, with the same stride */
+  int64_t k_stride, v_stride, q_stride, q_out_stride; /* elements from a token's rows to the next token's: at least heads * d, multiples of 8
+                                                       * (q, k and v may be slices of one projection's output); 0: heads * d */
+  const int32_t *positions; /* device [sum n_new] int32, the tokens' positions (any sign; not their places in the cache, which fall behind
+                             * them once KVCompress has dropped tokens); required with a rope, unused without */
+  const int32_t *n_cached;  /* host [B] >= 0: tokens of the sequence that the cache holds before the call */
+  const int32_t *n_new;     /* host [B] >= 0 */
+} fkv_new_tokens;
+
+/* The new tokens of each sequence into its pages behind the n_cached_b tokens there (serving counterpart of C <- update(K, V),
+ * Algorithm 1): logical tokens n_cached_b .. n_cached_b + n_new_b - 1 receive v and, turned by `rope` (NULL: as they are), k; q_out
+ * receives the queries turned the same way.  Pools and table as above; the sequences of a call must not write the same slot.  Other slots
+ * are not written; a table entry outside the pool writes nothing.  Needs no workspace: the context only names the device, and calls
+ * of one context on different streams may overlap.  Only n_seq and the head counts of `shape` are used. */
+int fkv_append_kv_paged(fkv_ctx *ctx, const fkv_shape *shape, const fkv_rope *rope, const fkv_new_tokens *tokens,
+                        const int32_t *block_table, int32_t max_pages_per_seq, int32_t page_size, int64_t n_pages,
+                        void *k_pages, void *v_pages, void *stream);
+
+/* Paged cache held in 8 bits (host struct).  A value is e4m3 (OCP FP8: 4 exponent bits, bias 7, 3 mantissa bits, no infinities, largest
+ * 448) times the scale of its block of scale_block tokens of one head:
+ *   k_pages, v_pages [n_pages][Hkv][page_size][d] uint8   one head's tokens of a page lie together (the bf16 pool's heads of a token do)
+ *   k_scale, v_scale [n_pages][Hkv][page_size / scale_block] fp32
+ * page_size is a power of two, at least 16; scale_block is 16, 32 or 64 and at most page_size; n_pages * page_size * Hkv < 2^31; the block
+ * table as above.  Nothing has to be cleared before first use.
+ *
+ * What the writing calls store, for the tokens X that a call puts into a block: p(a) = the smallest power of two >= 2^-126 with
+ * a <= 448 p(a), a = max |x| over the finite x of X.  A block without earlier tokens of the sequence takes the scale s' = p(a) whatever
+ * it held; one that earlier tokens lie in takes s' = max(s, p(a)), and where that is larger than its scale s the earlier codes become
+ * e4m3(code * s / s') (a power of two: exact, except where a code leaves e4m3's normal range).  X becomes e4m3(x / s'), rounded once, to
+ * nearest even; what is not finite becomes NaN.  Powers of two cost no precision, e4m3 being a floating format. */
+typedef struct fkv_quant_pages {
+  void *k_pages, *v_pages;
+  float *k_scale, *v_scale;
+  const int32_t *block_table; /* device [B][max_pages_per_seq] */
+  int32_t max_pages_per_seq, page_size, scale_block;
+  int64_t n_pages;
+} fkv_quant_pages;
+
+/* fkv_append_kv_paged, fkv_gather_kv_paged, fkv_compress_kv_paged and fkv_decode_attention_paged on such a cache.  Appending: the
+ * sequences of a call must not write into the same block.  Gathering: rows of negative indices are not written and do not count
+ * towards a scale.  A table entry outside the pool writes nothing, and is clamped into it by the decode call.
+ * Decoding: n_per_seq[b] >= 0, and a sequence without tokens gives zeros (the padding of a batch); any fp32 scales are read, not only powers
+ * of two.  Both contractions are accumulated in fp32 from exact products of what the codes stand for. */
+int fkv_append_kv_paged_quant(fkv_ctx *ctx, const fkv_shape *shape, const fkv_rope *rope, const fkv_new_tokens *tokens,
+                              const fkv_quant_pages *pages, void *stream);
+int fkv_gather_kv_paged_quant(fkv_ctx *ctx, const fkv_shape *shape, const void *k, const void *v, const int32_t *idx_kv,
+                              const int32_t *budget_per_seq, const fkv_quant_pages *pages, void *stream);
+int fkv_compress_kv_paged_quant(fkv_ctx *ctx, const fkv_shape *shape, const void *q_win, const void *k, const void *v,
+                                const int32_t *budget_per_seq, const fkv_quant_pages *pages, int32_t *idx_kv, void *stream);
+int fkv_decode_attention_paged_quant(fkv_ctx *ctx, const fkv_shape *shape, const void *q, const fkv_quant_pages *pages,
+                                     const int32_t *n_per_seq, float *out, void *stream);
+
 /* Measurement aid for callers that want the machine's achievable read bandwidth next to their
  * timings: one launch that only reads `bytes` (a multiple of 65536) of device memory at `src` with
  * the access pattern of the score kernels' K stream; streaming != 0 uses non-temporal loads.

@@ -29,6 +29,8 @@ EXPORTS = [
     "fkv_score_heads", "fkv_gather_kv_per_head", "fkv_count_from_rate", "fkv_decode_attention",
     "fkv_index_overlap", "fkv_mass_recall", "fkv_gather_kv_paged", "fkv_decode_attention_paged", "fkv_probe_read", "fkv_plan_layer", "fkv_set_wait_limit", "fkv_clear_error", "fkv_compress_kv_paged", "fkv_probe_logits", "fkv_window_output",
     "fkv_score_window_static", "fkv_score_plan", "fkv_score_window_output", "fkv_set_select_path",
+    "fkv_append_kv_paged", "fkv_append_kv_paged_quant", "fkv_gather_kv_paged_quant", "fkv_compress_kv_paged_quant",
+    "fkv_decode_attention_paged_quant",
 ]
 
 
@@ -41,6 +43,21 @@ class FkvShape(ctypes.Structure):
 
 class FkvLayerPlan(ctypes.Structure):
     _fields_ = [("tokens_in", ctypes.c_int32), ("k_tsp", ctypes.c_int32), ("kv_budget", ctypes.c_int32)]
+
+
+class FkvRope(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("inv_freq", ctypes.POINTER(ctypes.c_double))]
+
+
+class FkvNewTokens(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "q", "q_out")] + [
+        (n, ctypes.c_int64) for n in ("k_stride", "v_stride", "q_stride", "q_out_stride")] + [
+        ("positions", ctypes.c_void_p), ("n_cached", ctypes.POINTER(ctypes.c_int32)), ("n_new", ctypes.POINTER(ctypes.c_int32))]
+
+
+class FkvQuantPages(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_pages", "v_pages", "k_scale", "v_scale", "block_table")] + [
+        (n, ctypes.c_int32) for n in ("max_pages_per_seq", "page_size", "scale_block")] + [("n_pages", ctypes.c_int64)]
 
 
 class FkvError(RuntimeError):
@@ -98,6 +115,12 @@ def load():
     lib.fkv_gather_kv_paged.argtypes = [vp, shp, vp, vp, vp, pi32, vp, i32, i32, i64, vp, vp, vp]
     lib.fkv_compress_kv_paged.argtypes = [vp, shp, vp, vp, vp, pi32, vp, i32, i32, i64, vp, vp, vp, vp]
     lib.fkv_decode_attention_paged.argtypes = [vp, shp, vp, vp, vp, vp, i32, i32, i64, pi32, vp, vp]
+    rope, new, pages = ctypes.POINTER(FkvRope), ctypes.POINTER(FkvNewTokens), ctypes.POINTER(FkvQuantPages)
+    lib.fkv_append_kv_paged.argtypes = [vp, shp, rope, new, vp, i32, i32, i64, vp, vp, vp]
+    lib.fkv_append_kv_paged_quant.argtypes = [vp, shp, rope, new, pages, vp]
+    lib.fkv_gather_kv_paged_quant.argtypes = [vp, shp, vp, vp, vp, pi32, pages, vp]
+    lib.fkv_compress_kv_paged_quant.argtypes = [vp, shp, vp, vp, vp, pi32, pages, vp, vp]
+    lib.fkv_decode_attention_paged_quant.argtypes = [vp, shp, vp, pages, pi32, vp, vp]
     lib.fkv_plan_layer.argtypes = [i32, i32, i32, i32, ctypes.c_double, ctypes.c_double, i32, ctypes.POINTER(FkvLayerPlan)]
     lib.fkv_probe_logits.argtypes = [vp, shp, vp, vp, i32, vp, vp]
     lib.fkv_probe_read.argtypes = [vp, vp, i64, i32, vp]
@@ -117,7 +140,7 @@ def load():
     lib.fkv_profile_read.argtypes = [vp, ctypes.POINTER(ctypes.c_float), pi32, i32]
     for name in EXPORTS:
         getattr(lib, name)  # raises AttributeError if a declared symbol is missing
-    _native.bind(FkvShape, FkvError, {name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in EXPORTS})
+    _native.bind(FkvShape, FkvError, {name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in EXPORTS}, FkvRope)
     _lib = lib
     return lib
 
@@ -147,6 +170,31 @@ def make_shape(lengths, n_q_heads=32, n_kv_heads=8, head_dim=128, window=8, pool
     s._keep = arr
     s._lengths = [int(n) for n in lengths]
     return s
+
+
+def make_rope(rotary_dim=128, theta=10000.0, interleaved=False, inv_freq=None):
+    """Host descriptor of a rotary position embedding: the first rotary_dim columns of a row turn, pair i by position * inv_freq[i]
+    (theta ** (-2 i / rotary_dim) unless given); pairs are columns (i, i + rotary_dim / 2), or (2 i, 2 i + 1) if interleaved."""
+    freq = [theta ** (-2.0 * i / rotary_dim) for i in range(rotary_dim // 2)] if inv_freq is None else [float(f) for f in inv_freq]
+    if len(freq) != rotary_dim // 2:
+        raise ValueError("inv_freq holds %d frequencies, %d columns have %d pairs" % (len(freq), rotary_dim, rotary_dim // 2))
+    r = FkvRope()
+    arr = (ctypes.c_double * max(len(freq), 1))(*freq)
+    r.rotary_dim, r.interleaved = int(rotary_dim), int(bool(interleaved))
+    r.inv_freq = ctypes.cast(arr, ctypes.POINTER(ctypes.c_double))
+    r._keep = arr
+    return r
+
+
+def quant_pages(n_pages, page_size, n_kv_heads=8, head_dim=128, scale_block=16, device=None):
+    """Pools of a paged cache in 8 bits -> (k_pages, v_pages [n_pages, Hkv, page_size, d] float8_e4m3fn,
+    k_scale, v_scale [n_pages, Hkv, page_size / scale_block] fp32).  Their contents need no clearing: a block's scale is set with its first token."""
+    if scale_block < 1 or page_size % scale_block != 0:
+        raise ValueError("page_size %d is not a multiple of scale_block %d" % (page_size, scale_block))
+    dev = torch.device("cuda", torch.cuda.current_device()) if device is None else device
+    codes = [torch.empty((n_pages, n_kv_heads, page_size, head_dim), dtype=torch.float8_e4m3fn, device=dev) for _ in range(2)]
+    scales = [torch.empty((n_pages, n_kv_heads, page_size // scale_block), dtype=torch.float32, device=dev) for _ in range(2)]
+    return (*codes, *scales)
 
 
 def fkv_count_from_rate(n_tokens, rate):
@@ -215,6 +263,26 @@ class _Sizes:
 
 
 _BF16 = (torch.bfloat16, torch.int16, torch.uint16)
+_E4M3 = (torch.float8_e4m3fn, torch.uint8)
+
+
+def _token_rows(t, name, tokens, heads, dim, device):
+    """Pointer and token stride of [tokens, heads, d] rows that may be a slice of wider rows (heads side by side)."""
+    if tuple(t.shape) != (tokens, heads, dim):
+        raise ValueError("%s must be [%d, %d, %d], got %s" % (name, tokens, heads, dim, tuple(t.shape)))
+    if tokens == 0:
+        return None, 0
+    if not t.is_cuda:
+        raise ValueError("%s must be a GPU tensor" % name)
+    if t.device.index != device:
+        raise ValueError("%s is on cuda:%s, the context is on cuda:%d" % (name, t.device.index, device))
+    if t.dtype not in _BF16:
+        raise ValueError("%s has dtype %s, expected one of %s" % (name, t.dtype, _BF16))
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
+        raise ValueError("%s must have its heads side by side, got strides %s" % (name, tuple(t.stride())))
+    if tokens > 1 and t.stride(0) < heads * dim:
+        raise ValueError("the rows of %s overlap, got strides %s" % (name, tuple(t.stride())))
+    return t.data_ptr(), (t.stride(0) if tokens > 1 else 0)
 
 
 def _stream():
@@ -541,6 +609,137 @@ class Context:
                                                  kp, vp, bt, max_pages, page_size, n_pages, arr,
                                                  self._p(out, "out", (torch.float32,), numel=n.q_dec), _stream()),
                "fkv_decode_attention_paged")
+        return out
+
+    def _stream_here(self):
+        """The current stream, which must be the context's GPU's."""
+        if torch.cuda.current_device() != self.device:
+            raise ValueError("the current device is cuda:%d, the context is on cuda:%d" % (torch.cuda.current_device(), self.device))
+        return _stream()
+
+    def _new_tokens(self, shape, k, v, n_cached, n_new, rope, positions, q, q_out):
+        """Descriptor of the new tokens, their queries' output, and what has to live as long as the call."""
+        cached, c_arr = _counts(shape, n_cached)
+        new, n_arr = _counts(shape, n_new)
+        total, d = sum(new), shape.head_dim
+        if (q is None) and q_out is not None:
+            raise ValueError("q_out without q")
+        if rope is None and q is not None:
+            raise ValueError("q is there to be turned: it needs a rope")
+        if rope is not None and positions is None:
+            raise ValueError("a rope needs positions")
+        if rope is not None and not isinstance(rope, FkvRope):
+            raise ValueError("rope must come from make_rope, got %s" % type(rope).__name__)
+        t = FkvNewTokens()
+        t.k, t.k_stride = _token_rows(k, "k", total, shape.n_kv_heads, d, self.device)
+        t.v, t.v_stride = _token_rows(v, "v", total, shape.n_kv_heads, d, self.device)
+        if q is not None:
+            t.q, t.q_stride = _token_rows(q, "q", total, shape.n_q_heads, d, self.device)
+            if q_out is None:
+                q_out = torch.empty((total, shape.n_q_heads, d), dtype=q.dtype, device=q.device)
+            t.q_out, t.q_out_stride = _token_rows(q_out, "q_out", total, shape.n_q_heads, d, self.device)
+        if rope is not None:
+            t.positions = self._p(positions, "positions", (torch.int32,), numel=total)
+        t.n_cached, t.n_new = (ctypes.cast(a, ctypes.POINTER(ctypes.c_int32)) for a in (c_arr, n_arr))
+        t._keep = (c_arr, n_arr)
+        return t, q_out
+
+    def fkv_append_kv_paged(self, shape, k, v, n_cached, n_new, block_table, k_pages, v_pages, rope=None, positions=None, q=None,
+                            q_out=None):
+        """New tokens' rows into the pages behind the n_cached ones of their sequences: k, v [sum n_new,Hkv,d] bf16 (slices of a
+        projection's rows will do), k turned by `rope` (make_rope) at `positions` [sum n_new] int32; k_pages, v_pages
+        [n_pages,page_size,Hkv,d] are updated in place -> q [sum n_new,Hq,d], if given, turned likewise (q_out may be q)"""
+        done = _native.append_kv_paged(self._h, self.device, shape, k, v, n_cached, n_new, block_table, k_pages, v_pages, None, None, rope,
+                                       positions, q, q_out)
+        if done is not None:
+            return done[0]
+        t, q_out = self._new_tokens(shape, k, v, n_cached, n_new, rope, positions, q, q_out)
+        bt, max_pages, page_size, n_pages, kp, vp = self._paging(shape, block_table, k_pages, v_pages, True)
+        _check(load().fkv_append_kv_paged(self.handle, ctypes.byref(shape), rope and ctypes.byref(rope), ctypes.byref(t), bt, max_pages,
+                                          page_size, n_pages, kp, vp, self._stream_here()), "fkv_append_kv_paged")
+        return q_out
+
+    def _quant_pages(self, shape, block_table, k_pages, v_pages, k_scale, v_scale, v_required=True):
+        if block_table.dim() != 2 or block_table.shape[0] != shape.n_seq:
+            raise ValueError("block_table must be [n_seq, max_pages], got %s" % (tuple(block_table.shape),))
+        if k_pages.dim() != 4 or (k_pages.shape[1], k_pages.shape[3]) != (shape.n_kv_heads, shape.head_dim):
+            raise ValueError("k_pages must be [n_pages, Hkv, page_size, d], got %s" % (tuple(k_pages.shape),))
+        if k_scale is None or k_scale.dim() != 3 or tuple(k_scale.shape[:2]) != tuple(k_pages.shape[:2]) or k_scale.shape[2] < 1 \
+                or k_pages.shape[2] % k_scale.shape[2] != 0:
+            raise ValueError("k_scale must be [n_pages, Hkv, page_size / scale_block]")
+        for a, b, name in ((v_pages, k_pages, "v_pages"), (v_scale, k_scale, "v_scale")):
+            if a is not None and tuple(a.shape) != tuple(b.shape):
+                raise ValueError("%s must have the shape of %s" % (name, "k" + name[1:]))
+        p = FkvQuantPages()
+        p.k_pages, p.v_pages = self._p(k_pages, "k_pages", _E4M3), self._p(v_pages, "v_pages", _E4M3, not v_required)
+        p.k_scale = self._p(k_scale, "k_scale", (torch.float32,))
+        p.v_scale = self._p(v_scale, "v_scale", (torch.float32,), not v_required)
+        p.block_table = self._p(block_table, "block_table", (torch.int32,))
+        p.max_pages_per_seq, p.n_pages, p.page_size = int(block_table.shape[1]), int(k_pages.shape[0]), int(k_pages.shape[2])
+        p.scale_block = int(k_pages.shape[2] // k_scale.shape[2])
+        return p
+
+    def fkv_append_kv_paged_quant(self, shape, k, v, n_cached, n_new, block_table, k_pages, v_pages, k_scale, v_scale, rope=None,
+                                  positions=None, q=None, q_out=None):
+        """fkv_append_kv_paged into a cache in 8 bits (quant_pages): codes and scales are updated in place"""
+        done = _native.append_kv_paged(self._h, self.device, shape, k, v, n_cached, n_new, block_table, k_pages, v_pages, k_scale, v_scale, rope,
+                                       positions, q, q_out)
+        if done is not None:
+            return done[0]
+        t, q_out = self._new_tokens(shape, k, v, n_cached, n_new, rope, positions, q, q_out)
+        p = self._quant_pages(shape, block_table, k_pages, v_pages, k_scale, v_scale)
+        _check(load().fkv_append_kv_paged_quant(self.handle, ctypes.byref(shape), rope and ctypes.byref(rope), ctypes.byref(t), ctypes.byref(p),
+                                                self._stream_here()), "fkv_append_kv_paged_quant")
+        return q_out
+
+    def fkv_gather_kv_paged_quant(self, shape, k, v, idx_kv, budget_per_seq, block_table, k_pages, v_pages, k_scale, v_scale):
+        """fkv_gather_kv_paged into a cache in 8 bits (quant_pages), updated in place; v, v_pages and v_scale may be None"""
+        done = _native.gather_kv_paged_quant(self._h, self.device, shape, k, v, idx_kv, budget_per_seq, block_table, k_pages, v_pages, k_scale,
+                                             v_scale)
+        if done is not None:
+            return k_pages, v_pages, k_scale, v_scale
+        counts, arr = _counts(shape, budget_per_seq)
+        n = _Sizes(shape)
+        if len({v is None, v_pages is None, v_scale is None}) > 1:
+            raise ValueError("v, v_pages and v_scale go together")
+        p = self._quant_pages(shape, block_table, k_pages, v_pages, k_scale, v_scale, v is not None)
+        _check(load().fkv_gather_kv_paged_quant(self.handle, ctypes.byref(shape), self._p(k, "k", _BF16, numel=n.kv),
+                                                self._p(v, "v", _BF16, True, numel=n.kv),
+                                                self._p(idx_kv, "idx_kv", (torch.int32,), numel=shape.n_kv_heads * sum(counts)), arr,
+                                                ctypes.byref(p), self._stream_here()), "fkv_gather_kv_paged_quant")
+        return k_pages, v_pages, k_scale, v_scale
+
+    def fkv_compress_kv_paged_quant(self, shape, q_win, k, v, budget_per_seq, block_table, k_pages, v_pages, k_scale, v_scale, idx_kv=None):
+        """score -> per-KV-head select -> kept K/V rows into the pages in 8 bits; returns idx_kv [Hkv, sum budget]"""
+        done = _native.compress_kv_paged_quant(self._h, self.device, shape, q_win, k, v, budget_per_seq, block_table, k_pages, v_pages, k_scale,
+                                               v_scale, idx_kv)
+        if done is not None:
+            return done
+        counts, arr = _counts(shape, budget_per_seq)
+        n = _Sizes(shape)
+        if idx_kv is None:
+            idx_kv = torch.empty((shape.n_kv_heads, sum(counts)), dtype=torch.int32, device=k.device)
+        p = self._quant_pages(shape, block_table, k_pages, v_pages, k_scale, v_scale)
+        _check(load().fkv_compress_kv_paged_quant(self.handle, ctypes.byref(shape), self._p(q_win, "q_win", _BF16, numel=n.q_win),
+                                                  self._p(k, "k", _BF16, numel=n.kv), self._p(v, "v", _BF16, numel=n.kv), arr, ctypes.byref(p),
+                                                  self._p(idx_kv, "idx_kv", (torch.int32,), numel=shape.n_kv_heads * sum(counts)), self._stream_here()),
+               "fkv_compress_kv_paged_quant")
+        return idx_kv
+
+    def fkv_decode_attention_paged_quant(self, shape, q, k_pages, v_pages, k_scale, v_scale, block_table, n_per_seq, out=None):
+        """q [B,Hq,d] bf16 over a cache in 8 bits (quant_pages), block_table [B,max_pages] -> out [B,Hq,d] fp32; zeros for a sequence
+        without tokens"""
+        done = _native.decode_attention_paged_quant(self._h, self.device, shape, q, k_pages, v_pages, k_scale, v_scale, block_table, n_per_seq, out)
+        if done is not None:
+            return done
+        _, arr = _counts(shape, n_per_seq)
+        n = _Sizes(shape)
+        if out is None:
+            out = torch.empty((shape.n_seq, shape.n_q_heads, shape.head_dim), dtype=torch.float32, device=q.device)
+        p = self._quant_pages(shape, block_table, k_pages, v_pages, k_scale, v_scale)
+        _check(load().fkv_decode_attention_paged_quant(self.handle, ctypes.byref(shape), self._p(q, "q", _BF16, numel=n.q_dec), ctypes.byref(p),
+                                                       arr, self._p(out, "out", (torch.float32,), numel=n.q_dec), self._stream_here()),
+               "fkv_decode_attention_paged_quant")
         return out
 
     def fkv_probe_read(self, src, streaming=False):

@@ -1175,6 +1175,261 @@ int fkv_compress_kv_paged(fkv_ctx *ctx, const fkv_shape *shape, const void *q_wi
   return enqueue_gather_paged(ctx, r, g, k, v, idx_kv, pg, k_pages, v_pages, st);
 }
 
+namespace {
+// A paged cache held in 8 bits: geometry and pointers; without V where `v_optional`.
+int check_quant_pages(const fkv_quant_pages *p, int Hkv, bool v_optional, Paging *pg) {
+  if (!p || !p->k_pages || !p->k_scale) return FKV_ENULL;
+  if ((p->v_pages == nullptr) != (p->v_scale == nullptr) || (!p->v_pages && !v_optional)) return FKV_ENULL;
+  *pg = Paging{p->block_table, p->max_pages_per_seq, p->page_size, p->n_pages};
+  const int rc = check_paging(*pg, Hkv);
+  if (rc != FKV_OK) return rc;
+  if (p->scale_block != 16 && p->scale_block != 32 && p->scale_block != 64) return FKV_EINVAL;
+  if (p->page_size < p->scale_block) return FKV_EINVAL;
+  if (misaligned(p->k_pages) || misaligned(p->v_pages) || misaligned(p->k_scale) || misaligned(p->v_scale)) return FKV_EALIGN;
+  return FKV_OK;
+}
+
+// Elements between the rows of two tokens: `given`, or heads * d.
+int check_stride(int64_t given, int heads, int64_t *out) {
+  *out = given == 0 ? (int64_t)heads * kHeadDim : given;
+  if (*out < (int64_t)heads * kHeadDim || *out > INT32_MAX) return FKV_EINVAL;
+  return *out % 8 != 0 ? FKV_EALIGN : FKV_OK;
+}
+
+constexpr int64_t kAppendMaxTokens = 1 << 28;  // block numbers of a launch stay below 2^31
+
+int fill_append(const Resolved &r, const fkv_rope *rope, const fkv_new_tokens *t, const Paging &pg, AppendArgs *a) {
+  if (!t || !t->n_cached || !t->n_new) return FKV_ENULL;
+  int64_t total = 0;
+  a->off[0] = 0;
+  for (int b = 0; b < r.n_seq; ++b) {
+    if (t->n_cached[b] < 0 || t->n_new[b] < 0) return FKV_EINVAL;
+    if ((int64_t)t->n_cached[b] + t->n_new[b] > (int64_t)pg.max_pages * pg.page_size) return FKV_EINVAL;
+    total += t->n_new[b];
+    if (total > kAppendMaxTokens) return FKV_EINVAL;
+    a->start[b] = t->n_cached[b];
+    a->off[b + 1] = (int)total;
+  }
+  a->total = (int)total;
+  if (rope) {
+    if (rope->rotary_dim < 16 || rope->rotary_dim > kHeadDim || rope->rotary_dim % 16 != 0) return FKV_EINVAL;
+    if (rope->interleaved != 0 && rope->interleaved != 1) return FKV_EINVAL;
+    if (!rope->inv_freq) return FKV_ENULL;
+    a->pairs = rope->rotary_dim / 2;
+    a->interleaved = rope->interleaved;
+    for (int i = 0; i < a->pairs; ++i) {
+      if (!isfinite(rope->inv_freq[i])) return FKV_EINVAL;
+      long double turns = (long double)rope->inv_freq[i] / 6.283185307179586476925286766559L;
+      turns = floorl(ldexpl(turns - floorl(turns), 64) + 0.5L);
+      a->freq[i] = turns < 18446744073709551616.0L ? (uint64_t)turns : 0;  // a whole turn is none
+    }
+  } else if (t->q || t->q_out) {
+    return FKV_EINVAL;  // queries are only there to be turned
+  }
+  int rc = check_stride(t->k_stride, r.Hkv, &a->k_stride);
+  if (rc == FKV_OK) rc = check_stride(t->v_stride, r.Hkv, &a->v_stride);
+  if (rc == FKV_OK) rc = check_stride(t->q_stride, r.Hq, &a->q_stride);
+  if (rc == FKV_OK) rc = check_stride(t->q_out_stride, r.Hq, &a->q_out_stride);
+  if (rc != FKV_OK) return rc;
+  if (total > 0) {
+    if (!t->k || !t->v || (t->q == nullptr) != (t->q_out == nullptr) || (rope && !t->positions)) return FKV_ENULL;
+    if (t->q && t->q_out == t->q && a->q_stride != a->q_out_stride) return FKV_EINVAL;
+    if (misaligned(t->k) || misaligned(t->v) || misaligned(t->q) || misaligned(t->q_out)) return FKV_EALIGN;
+  }
+  a->q = static_cast<const uint16_t *>(t->q);
+  a->k = static_cast<const uint16_t *>(t->k);
+  a->v = static_cast<const uint16_t *>(t->v);
+  a->q_out = static_cast<uint16_t *>(t->q_out);
+  a->positions = t->positions;
+  a->Hq = r.Hq;
+  a->Hkv = r.Hkv;
+  a->n_seq = r.n_seq;
+  a->block_table = pg.table;
+  a->max_pages = pg.max_pages;
+  a->page_shift = log2_exact(pg.page_size);
+  a->n_pages = (int)pg.n_pages;
+  return FKV_OK;
+}
+
+void fill_gather_quant(QuantGatherArgs &g, const Resolved &r, const void *k, const void *v, const int32_t *idx_kv, const fkv_quant_pages *p) {
+  g.src[0] = static_cast<const uint16_t *>(k);
+  g.src[1] = static_cast<const uint16_t *>(v);
+  g.codes[0] = static_cast<uint8_t *>(p->k_pages);
+  g.codes[1] = static_cast<uint8_t *>(p->v_pages);
+  g.scale[0] = p->k_scale;
+  g.scale[1] = p->v_scale;
+  g.idx = idx_kv;
+  g.block_table = p->block_table;
+  g.max_pages = p->max_pages_per_seq;
+  g.page_shift = log2_exact(p->page_size);
+  g.n_pages = (int)p->n_pages;
+  g.Hkv = r.Hkv;
+  g.total_rows = g.cnt_off[r.n_seq];
+  g.n_seq = r.n_seq;
+  g.blk[0] = 0;
+  for (int b = 0; b < r.n_seq; ++b) g.blk[b + 1] = g.blk[b] + (g.cnt_off[b + 1] - g.cnt_off[b] + p->scale_block - 1) / p->scale_block;
+  for (int b = 0; b <= r.n_seq; ++b) g.cu[b] = r.cu[b];
+}
+
+int check_budget_pages(const Resolved &r, const int32_t *budget_per_seq, const Paging &pg) {
+  for (int b = 0; b < r.n_seq; ++b)
+    if (budget_per_seq[b] > (int64_t)pg.max_pages * pg.page_size) return FKV_EINVAL;
+  return FKV_OK;
+}
+}  // namespace
+
+int fkv_append_kv_paged(fkv_ctx *ctx, const fkv_shape *shape, const fkv_rope *rope, const fkv_new_tokens *tokens,
+                        const int32_t *block_table, int32_t max_pages_per_seq, int32_t page_size, int64_t n_pages,
+                        void *k_pages, void *v_pages, void *stream) {
+  Resolved r;
+  int rc = resolve(shape, &r);
+  if (rc != FKV_OK) return rc;
+  if (!k_pages || !v_pages) return FKV_ENULL;
+  const Paging pg{block_table, max_pages_per_seq, page_size, n_pages};
+  rc = check_paging(pg, r.Hkv);
+  if (rc != FKV_OK) return rc;
+  AppendArgs a{};
+  rc = fill_append(r, rope, tokens, pg, &a);
+  if (rc != FKV_OK) return rc;
+  if (misaligned(k_pages) || misaligned(v_pages)) return FKV_EALIGN;
+  if (!ctx) return FKV_ENULL;
+  ctx->ev_prev = nullptr;
+  if (a.total == 0) return FKV_OK;
+  a.k_pages = static_cast<uint16_t *>(k_pages);
+  a.v_pages = static_cast<uint16_t *>(v_pages);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  Timed t(ctx, st, KID_GATHER);
+  const hipError_t e = launch_append(a, st);
+  return e == hipSuccess ? FKV_OK : hip_fail(e);
+}
+
+int fkv_append_kv_paged_quant(fkv_ctx *ctx, const fkv_shape *shape, const fkv_rope *rope, const fkv_new_tokens *tokens,
+                              const fkv_quant_pages *pages, void *stream) {
+  Resolved r;
+  int rc = resolve(shape, &r);
+  if (rc != FKV_OK) return rc;
+  Paging pg;
+  rc = check_quant_pages(pages, r.Hkv, false, &pg);
+  if (rc != FKV_OK) return rc;
+  AppendArgs a{};
+  rc = fill_append(r, rope, tokens, pg, &a);
+  if (rc != FKV_OK) return rc;
+  if (!ctx) return FKV_ENULL;
+  ctx->ev_prev = nullptr;
+  if (a.total == 0) return FKV_OK;
+  const int block = pages->scale_block;
+  for (int b = 0; b < r.n_seq; ++b) {
+    const int n = a.off[b + 1] - a.off[b];
+    a.blk[b + 1] = a.blk[b] + (n > 0 ? (a.start[b] + n - 1) / block - a.start[b] / block + 1 : 0);
+  }
+  a.k_codes = static_cast<uint8_t *>(pages->k_pages);
+  a.v_codes = static_cast<uint8_t *>(pages->v_pages);
+  a.k_scale = pages->k_scale;
+  a.v_scale = pages->v_scale;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  Timed t(ctx, st, KID_GATHER);
+  const hipError_t e = launch_append_quant(a, block, st);
+  return e == hipSuccess ? FKV_OK : hip_fail(e);
+}
+
+int fkv_gather_kv_paged_quant(fkv_ctx *ctx, const fkv_shape *shape, const void *k, const void *v, const int32_t *idx_kv,
+                              const int32_t *budget_per_seq, const fkv_quant_pages *pages, void *stream) {
+  Resolved r;
+  int rc = resolve(shape, &r);
+  if (rc != FKV_OK) return rc;
+  if (!k || !idx_kv) return FKV_ENULL;
+  Paging pg;
+  rc = check_quant_pages(pages, r.Hkv, true, &pg);
+  if (rc != FKV_OK) return rc;
+  if ((v == nullptr) != (pages->v_pages == nullptr)) return FKV_ENULL;
+  QuantGatherArgs g{};
+  rc = check_counts(r, budget_per_seq, g.cnt_off);
+  if (rc == FKV_OK) rc = check_budget_pages(r, budget_per_seq, pg);
+  if (rc != FKV_OK) return rc;
+  if (misaligned(k) || misaligned(v) || misaligned(idx_kv)) return FKV_EALIGN;
+  rc = check_ctx(ctx, r);
+  if (rc != FKV_OK) return rc;
+  fill_gather_quant(g, r, k, v, idx_kv, pages);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  Timed t(ctx, st, KID_GATHER);
+  const hipError_t e = launch_gather_quant(g, pages->scale_block, st);
+  return e == hipSuccess ? FKV_OK : hip_fail(e);
+}
+
+int fkv_compress_kv_paged_quant(fkv_ctx *ctx, const fkv_shape *shape, const void *q_win, const void *k, const void *v,
+                                const int32_t *budget_per_seq, const fkv_quant_pages *pages, int32_t *idx_kv, void *stream) {
+  Resolved r;
+  int rc = resolve(shape, &r);
+  if (rc != FKV_OK) return rc;
+  if (!q_win || !k || !v || !idx_kv) return FKV_ENULL;
+  Paging pg;
+  rc = check_quant_pages(pages, r.Hkv, false, &pg);
+  if (rc != FKV_OK) return rc;
+  QuantGatherArgs g{};
+  rc = check_counts(r, budget_per_seq, g.cnt_off);
+  if (rc == FKV_OK) rc = check_budget_pages(r, budget_per_seq, pg);
+  if (rc != FKV_OK) return rc;
+  if (misaligned(q_win) || misaligned(k) || misaligned(v) || misaligned(idx_kv)) return FKV_EALIGN;
+  rc = check_ctx(ctx, r);
+  if (rc != FKV_OK) return rc;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  float *sg = reinterpret_cast<float *>(ctx->ws + ctx->lay.scores_group);
+  SelectArgs sel{};
+  fill_select(sel, ctx, r);
+  fill_rowset(&sel.set[sel.n_sets++], sg, r.sum_p, r.Hkv, idx_kv, g.cnt_off, r.n_seq);
+  rc = enqueue_score(ws_of(ctx), shape, r, q_win, k, sg, nullptr, nullptr, st);
+  if (rc != FKV_OK) return rc;
+  hipError_t e = enqueue_select(ctx, sel, st);
+  if (e != hipSuccess) return hip_fail(e);
+  fill_gather_quant(g, r, k, v, idx_kv, pages);
+  Timed t(ctx, st, KID_GATHER);
+  e = launch_gather_quant(g, pages->scale_block, st);
+  return e == hipSuccess ? FKV_OK : hip_fail(e);
+}
+
+int fkv_decode_attention_paged_quant(fkv_ctx *ctx, const fkv_shape *shape, const void *q, const fkv_quant_pages *pages,
+                                     const int32_t *n_per_seq, float *out, void *stream) {
+  Resolved r;
+  int rc = resolve(shape, &r);
+  if (rc != FKV_OK) return rc;
+  if (!q || !n_per_seq || !out) return FKV_ENULL;
+  Paging pg;
+  rc = check_quant_pages(pages, r.Hkv, false, &pg);
+  if (rc != FKV_OK) return rc;
+  DecodeQuantArgs a{};
+  int64_t tot = 0;
+  for (int b = 0; b < r.n_seq; ++b) {
+    if (n_per_seq[b] < 0 || n_per_seq[b] > (int64_t)pg.max_pages * pg.page_size) return FKV_EINVAL;
+    tot += n_per_seq[b];
+    if (tot > INT32_MAX) return FKV_EINVAL;
+    a.d.off[b + 1] = (int)tot;
+  }
+  if (misaligned(q) || misaligned(out)) return FKV_EALIGN;
+  if (!ctx) return FKV_ENULL;
+  if (r.n_seq > ctx->max_seqs) return FKV_EWORKSPACE;
+  ctx->ev_prev = nullptr;
+  a.d.q = static_cast<const uint16_t *>(q);
+  a.d.out = out;
+  a.d.part = reinterpret_cast<float *>(ctx->ws + ctx->lay.dec_part);
+  a.d.count = reinterpret_cast<unsigned *>(ctx->ws + ctx->lay.dec_count);
+  a.d.block_table = pg.table;
+  a.d.max_pages = pg.max_pages;
+  a.d.page_shift = log2_exact(pg.page_size);
+  a.d.n_pages = (int)pg.n_pages;
+  a.d.Hq = r.Hq; a.d.Hkv = r.Hkv; a.d.G = r.G; a.d.n_seq = r.n_seq;
+  const float scale = shape->softmax_scale > 0.f ? shape->softmax_scale : 1.0f / sqrtf((float)shape->head_dim);
+  a.d.scale_log2e = scale * 1.4426950408889634f;
+  a.k = static_cast<const uint8_t *>(pages->k_pages);
+  a.v = static_cast<const uint8_t *>(pages->v_pages);
+  a.k_scale = pages->k_scale;
+  a.v_scale = pages->v_scale;
+  a.block_shift = log2_exact(pages->scale_block);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  Timed t(ctx, st, KID_DECODE);
+  const hipError_t e = launch_decode_quant(a, ctx->n_cu > 0 ? ctx->n_cu : 256, st);
+  return e == hipSuccess ? FKV_OK : hip_fail(e);
+}
+
 int fkv_probe_read(fkv_ctx *ctx, const void *src, int64_t bytes, int32_t streaming, void *stream) {
   if (bytes < 0 || (bytes & 65535) != 0 || bytes / 65536 > INT32_MAX) return FKV_EINVAL;
   if (!src && bytes > 0) return FKV_ENULL;

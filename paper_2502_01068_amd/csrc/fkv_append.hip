@@ -1,0 +1,291 @@
+// New tokens' keys and values into a paged cache, rotary position embedding applied to the keys and queries on the way; and the
+// writing side of the cache in 8 bits: appending to it, and KVCompress (App. B.1) into it.
+//
+// Rotation: (x, y) -> (x cos - y sin, y cos + x sin), phi = position * inv_freq[i].  Angles are held in turns as 64-bit whole numbers (2^64 = one
+// turn): position * freq wraps around by itself, which reduces the angle exactly however far the position.  The top 32 bits become an
+// fp32 number of half turns in [-1, 1], good to 2^-25.  A block forms sine and cosine of its tokens once, in LDS, for all heads.
+//
+// A thread handles 16 columns of a row: two 16-byte chunks, which hold both columns of its 8 pairs (adjacent chunks, or chunks i and
+// i + r/16 where pairs are half the turned columns apart); 8 threads make a row.
+#include "fkv_quant.h"
+
+namespace fkv {
+
+constexpr int kAppendThreads = 256;
+constexpr int kRowLanes = 8;  // threads of a row
+constexpr int kPairs = kHeadDim / 2;
+
+// sine and cosine of a block's tokens, a row of kPairs each
+template <int kTok>
+struct TurnTable {
+  float cs[kTok][kPairs], sn[kTok][kPairs];
+};
+
+// Fills rows 0 .. n - 1 of the table for the packed tokens token0, token0 + 1, ..; all threads of the block.
+template <int kTok>
+__device__ __forceinline__ void fill_turns(const AppendArgs &a, TurnTable<kTok> &t, int token0, int n) {
+  for (int e = threadIdx.x; e < n * kPairs; e += blockDim.x) {
+    const int tok = e / kPairs, i = e % kPairs;
+    if (i < a.pairs) {
+      const uint64_t turns = (uint64_t)(int64_t)a.positions[token0 + tok] * a.freq[i];
+      sincospif((float)(int32_t)(turns >> 32) * 0x1p-31f, &t.sn[tok][i], &t.cs[tok][i]);
+    }
+  }
+}
+
+// Where a thread's two chunks of a row lie; turned: they hold pairs 8 j .. 8 j + 7.
+struct RowPart {
+  int first, second;
+  bool turned;
+};
+__device__ __forceinline__ RowPart row_part(const AppendArgs &a, int j, bool rotate) {
+  const int n_turn = a.pairs / 8;
+  RowPart p{2 * j, 2 * j + 1, rotate && j < n_turn};
+  if (p.turned && !a.interleaved) {
+    p.first = j;
+    p.second = j + n_turn;
+  }
+  return p;
+}
+
+// The 16 values of a thread's chunks, turned by the pairs' angles.
+__device__ __forceinline__ void turn16(const AppendArgs &a, u32x4 first, u32x4 second, const float *cs, const float *sn, float (&x)[16]) {
+  float v[16], c[8], s[8];
+  unpack8(first, v);
+  unpack8(second, v + 8);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) c[i] = cs[i], s[i] = sn[i];
+  if (a.interleaved) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      x[2 * i] = v[2 * i] * c[i] - v[2 * i + 1] * s[i];
+      x[2 * i + 1] = v[2 * i + 1] * c[i] + v[2 * i] * s[i];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      x[i] = v[i] * c[i] - v[8 + i] * s[i];
+      x[8 + i] = v[8 + i] * c[i] + v[i] * s[i];
+    }
+  }
+}
+
+__device__ __forceinline__ int seq_at(const int *off, int n_seq, int i) {  // the sequence that entry i of a packed batch belongs to
+  int b = 0;
+  while (b + 1 < n_seq && i >= off[b + 1]) ++b;
+  return b;
+}
+
+// The rows of kTok tokens: queries (n_q heads, into q_out), keys and values (n_kv heads each, into the pages).
+template <int kTok>
+__device__ __forceinline__ void append_rows(const AppendArgs &a, TurnTable<kTok> &turns, int (&slots)[kTok], int token0, int n_q, int n_kv) {
+  const int n_tok = min(kTok, a.total - token0), tid = threadIdx.x, j = tid & (kRowLanes - 1);
+  const int rows_per = n_q + 2 * n_kv, n_rows = n_tok * rows_per;
+  struct Row {
+    int tok, h, kind;  // kind 0: query, 1: key, 2: value
+    const u32x4 *src;
+    RowPart part;
+  };
+  auto row_at = [&](int r) {
+    Row w;
+    w.tok = kTok == 1 ? 0 : r / rows_per;
+    w.h = r - w.tok * rows_per;
+    w.kind = w.h < n_q ? 0 : w.h < n_q + n_kv ? 1 : 2;
+    w.h -= w.kind == 0 ? 0 : w.kind == 1 ? n_q : n_q + n_kv;
+    const uint16_t *base = w.kind == 0 ? a.q : w.kind == 1 ? a.k : a.v;
+    const int64_t stride = w.kind == 0 ? a.q_stride : w.kind == 1 ? a.k_stride : a.v_stride;
+    w.src = reinterpret_cast<const u32x4 *>(base + (int64_t)(token0 + w.tok) * stride + w.h * kHeadDim);
+    w.part = row_part(a, j, w.kind != 2);
+    return w;
+  };
+  if (n_kv > 0 && tid < n_tok) {
+    const int t = token0 + tid, b = seq_at(a.off, a.n_seq, t), at = a.start[b] + (t - a.off[b]);
+    const int page = a.block_table[(size_t)b * a.max_pages + (at >> a.page_shift)];
+    slots[tid] = page >= 0 && page < a.n_pages ? (page << a.page_shift) + (at & ((1 << a.page_shift) - 1)) : -1;
+  }
+  if (a.pairs > 0) fill_turns(a, turns, token0, n_tok);
+  __syncthreads();
+  for (int r = tid / kRowLanes; r < n_rows; r += blockDim.x / kRowLanes) {
+    const Row w = row_at(r);
+    u32x4 first = w.src[w.part.first], second = w.src[w.part.second];
+    if (w.part.turned) {
+      float x[16];
+      turn16(a, first, second, &turns.cs[w.tok][8 * j], &turns.sn[w.tok][8 * j], x);
+      first = pack8(x);
+      second = pack8(x + 8);
+    }
+    u32x4 *dst;
+    if (w.kind == 0) {
+      dst = reinterpret_cast<u32x4 *>(a.q_out + (int64_t)(token0 + w.tok) * a.q_out_stride + w.h * kHeadDim);
+    } else {
+      const int slot = slots[w.tok];
+      if (slot < 0) continue;
+      dst = reinterpret_cast<u32x4 *>((w.kind == 1 ? a.k_pages : a.v_pages) + ((size_t)slot * a.Hkv + w.h) * kHeadDim);
+    }
+    dst[w.part.first] = first;
+    dst[w.part.second] = second;
+  }
+}
+
+template <int kTok>
+__global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a) {
+  __shared__ __attribute__((aligned(16))) TurnTable<kTok> turns;
+  __shared__ int slots[kTok];
+  append_rows<kTok>(a, turns, slots, blockIdx.x * kTok, a.q ? a.Hq : 0, a.Hkv);
+}
+
+// One scale block of one head, a wave's work: of its rows 0 .. kBlock - 1 (of kHeadDim bytes at `codes`) first .. last - 1 may be new, and
+// earlier tokens lie in those ahead of them.  A thread has row p * kRowLanes + lane / kRowLanes of step p.  live(p): that row is
+// new indeed; load(p, chunks) fetches its two 16-byte chunks, value(p, chunks, x) gives their 16 numbers.  No new row: nothing is written.
+template <int kBlock, typename Live, typename Load, typename Value>
+__device__ __forceinline__ void store_block(int first, int last, uint8_t *codes, float *scale, Live live, Load load, Value value, RowPart part) {
+  constexpr int kSteps = kBlock / kRowLanes;
+  const int lane = threadIdx.x & 63, j = lane & (kRowLanes - 1), sub = lane / kRowLanes;
+  u32x4 raw[kSteps][2];
+  bool is_new[kSteps], any = false;
+#pragma unroll
+  for (int p = 0; p < kSteps; ++p) {
+    const int i = p * kRowLanes + sub;
+    is_new[p] = i >= first && i < last && live(p);
+    any |= is_new[p];
+    if (is_new[p]) load(p, raw[p]);
+  }
+  float amax = 0.f;
+#pragma unroll
+  for (int p = 0; p < kSteps; ++p) {
+    if (is_new[p]) {
+      float x[16];
+      value(p, raw[p], x);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) amax = fmaxf(amax, is_finite(x[e]) ? __builtin_fabsf(x[e]) : 0.f);
+    }
+  }
+  if (__builtin_amdgcn_ballot_w64(any) == 0ull) return;
+  amax = wave_fmax(amax);
+  const float old = first > 0 ? *scale : 0.f, now = fmaxf(scale_for(amax), old), inv = 1.f / now;
+  if (first > 0 && now > old) {
+    const float ratio = old / now;
+    for (int i = sub; i < first; i += kRowLanes) {
+      u32x4 *row = reinterpret_cast<u32x4 *>(codes + i * kHeadDim) + j;
+      u32x4 c = *row;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) c[e] = rescale4(c[e], ratio);
+      *row = c;
+    }
+  }
+#pragma unroll
+  for (int p = 0; p < kSteps; ++p) {
+    if (is_new[p]) {
+      float x[16];
+      value(p, raw[p], x);
+      u32x2 *row = reinterpret_cast<u32x2 *>(codes + (p * kRowLanes + sub) * kHeadDim);
+      row[part.first] = encode8(x, inv);
+      row[part.second] = encode8(x + 8, inv);
+    }
+  }
+  if (lane == 0) *scale = now;
+}
+
+// Blocks of the grid: a scale block of a sequence for K, one for V (a wave for each head), and so on, then kAppendTok tokens' queries each.
+constexpr int kAppendTok = 8;
+
+template <int kBlock>
+__global__ __launch_bounds__(kMaxKvHeads * 64) void k_append_quant(AppendArgs a) {
+  constexpr int kTok = kBlock > kAppendTok ? kBlock : kAppendTok;
+  __shared__ __attribute__((aligned(16))) TurnTable<kTok> turns;
+  const int block = blockIdx.x, n_blk = 2 * a.blk[a.n_seq];
+  if (block >= n_blk) {
+    __shared__ int slots[kAppendTok];
+    append_rows<kAppendTok>(a, reinterpret_cast<TurnTable<kAppendTok> &>(turns), slots, (block - n_blk) * kAppendTok, a.Hq, 0);
+    return;
+  }
+  const bool is_v = (block & 1) != 0;
+  const int at = block >> 1, b = seq_at(a.blk, a.n_seq, at);
+  const int start = a.start[b], end = start + (a.off[b + 1] - a.off[b]);
+  const int tok0 = (start / kBlock + (at - a.blk[b])) * kBlock;  // the block's first token
+  const int first = max(start - tok0, 0), last = min(end - tok0, kBlock);
+  const int page = a.block_table[(size_t)b * a.max_pages + (tok0 >> a.page_shift)];
+  const int token0 = a.off[b] + (tok0 + first - start);  // packed index of the first new token
+  const bool turn = !is_v && a.pairs > 0;
+  if (turn) {
+    fill_turns(a, turns, token0, last - first);
+    __syncthreads();
+  }
+  if (page < 0 || page >= a.n_pages) return;
+  const int h = threadIdx.x >> 6, lane = threadIdx.x & 63, j = lane & (kRowLanes - 1), in_page = tok0 & ((1 << a.page_shift) - 1);
+  const size_t row = (((size_t)page * a.Hkv + h) << a.page_shift) + in_page;
+  const RowPart part = row_part(a, j, turn);
+  const uint16_t *src = (is_v ? a.v : a.k) + h * kHeadDim;
+  const int64_t stride = is_v ? a.v_stride : a.k_stride;
+  const int sub = lane / kRowLanes - first;  // of a thread's row among the new ones, in step 0
+  store_block<kBlock>(
+      first, last, (is_v ? a.v_codes : a.k_codes) + row * kHeadDim, (is_v ? a.v_scale : a.k_scale) + row / kBlock,
+      [](int) { return true; },
+      [&](int p, u32x4 (&raw)[2]) {
+        const u32x4 *r = reinterpret_cast<const u32x4 *>(src + (int64_t)(token0 + p * kRowLanes + sub) * stride);
+        raw[0] = r[part.first];
+        raw[1] = r[part.second];
+      },
+      [&](int p, const u32x4 (&raw)[2], float (&x)[16]) {
+        if (part.turned) {
+          const int i = p * kRowLanes + sub;
+          turn16(a, raw[0], raw[1], &turns.cs[i][8 * j], &turns.sn[i][8 * j], x);
+        } else {
+          unpack8(raw[0], x);
+          unpack8(raw[1], x + 8);
+        }
+      },
+      part);
+}
+
+// KVCompress into the cache in 8 bits: block (scale block of kept rows, K or V), a wave for each head.
+template <int kBlock>
+__global__ __launch_bounds__(kMaxKvHeads * 64) void k_gather_quant(QuantGatherArgs a) {
+  const int at = blockIdx.x, b = seq_at(a.blk, a.n_seq, at), is_v = blockIdx.y;
+  const int tok0 = (at - a.blk[b]) * kBlock, last = min(a.cnt_off[b + 1] - a.cnt_off[b] - tok0, kBlock);
+  const int page = a.block_table[(size_t)b * a.max_pages + (tok0 >> a.page_shift)];
+  if (page < 0 || page >= a.n_pages) return;
+  const int h = threadIdx.x >> 6, lane = threadIdx.x & 63, j = lane & (kRowLanes - 1), in_page = tok0 & ((1 << a.page_shift) - 1);
+  const size_t row = (((size_t)page * a.Hkv + h) << a.page_shift) + in_page;
+  const int base = a.cu[b], n = a.cu[b + 1] - base;
+  const int all = a.idx[(size_t)h * a.total_rows + a.cnt_off[b] + tok0 + min(lane & (kBlock - 1), last - 1)];  // a lane each
+  int kept[kBlock / kRowLanes];
+#pragma unroll
+  for (int p = 0; p < kBlock / kRowLanes; ++p) kept[p] = __shfl(all, p * kRowLanes + lane / kRowLanes);
+  const uint16_t *src = a.src[is_v] + h * kHeadDim;
+  store_block<kBlock>(
+      0, last, a.codes[is_v] + row * kHeadDim, a.scale[is_v] + row / kBlock, [&](int p) { return kept[p] >= 0; },
+      [&](int p, u32x4 (&raw)[2]) {
+        const u32x4 *r = reinterpret_cast<const u32x4 *>(src + (int64_t)(base + min(kept[p], n - 1)) * a.Hkv * kHeadDim);
+        raw[0] = r[2 * j];
+        raw[1] = r[2 * j + 1];
+      },
+      [&](int, const u32x4 (&raw)[2], float (&x)[16]) {
+        unpack8(raw[0], x);
+        unpack8(raw[1], x + 8);
+      },
+      RowPart{2 * j, 2 * j + 1, false});
+}
+
+hipError_t launch_append(const AppendArgs &a, hipStream_t s) {
+  hipLaunchKernelGGL((k_append<1>), dim3(a.total), dim3(kAppendThreads), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_append_quant(const AppendArgs &a, int block, hipStream_t s) {
+  const dim3 grid(2 * a.blk[a.n_seq] + (a.q ? (a.total + kAppendTok - 1) / kAppendTok : 0)), threads(a.Hkv * 64);
+  if (block == 16) hipLaunchKernelGGL((k_append_quant<16>), grid, threads, 0, s, a);
+  else if (block == 32) hipLaunchKernelGGL((k_append_quant<32>), grid, threads, 0, s, a);
+  else hipLaunchKernelGGL((k_append_quant<64>), grid, threads, 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_gather_quant(const QuantGatherArgs &a, int block, hipStream_t s) {
+  const dim3 grid(a.blk[a.n_seq], a.src[1] ? 2 : 1), threads(a.Hkv * 64);
+  if (block == 16) hipLaunchKernelGGL((k_gather_quant<16>), grid, threads, 0, s, a);
+  else if (block == 32) hipLaunchKernelGGL((k_gather_quant<32>), grid, threads, 0, s, a);
+  else hipLaunchKernelGGL((k_gather_quant<64>), grid, threads, 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace fkv

@@ -224,6 +224,16 @@ struct DecodeArgs {
 };
 hipError_t launch_decode(DecodeArgs &a, int n_cu, hipStream_t s);
 
+// The same over a cache held in 8 bits: page pools [n_pages][Hkv][page_size][d] of e4m3 codes, a scale for every 1 << block_shift tokens
+// of a page and head.  Of `d` the queries, the output, the workspace, the head counts, the sequences and the block table are used.
+struct DecodeQuantArgs {
+  DecodeArgs d;
+  const uint8_t *k, *v;
+  const float *k_scale, *v_scale;
+  int block_shift;
+};
+hipError_t launch_decode_quant(DecodeQuantArgs &a, int n_cu, hipStream_t s);
+
 // ---- attention output of the window rows ------------------------------------------------
 constexpr int kWoutBlocks = 256;  // blocks a launch aims for (one per CU: 128 KiB of LDS each)
 struct WoutArgs {
@@ -321,6 +331,41 @@ struct PagedGatherArgs {
   int cnt_off[FKV_MAX_SEQS + 1];
 };
 hipError_t launch_gather_paged(const PagedGatherArgs &a, hipStream_t s);
+// KVCompress into a cache held in 8 bits: pages [n_pages][Hkv][page_size][d] of codes, a scale per block of tokens and head.
+struct QuantGatherArgs {
+  const uint16_t *src[2];       // K, V: [sum L][Hkv][d] bf16 (V may be nullptr)
+  uint8_t *codes[2];
+  float *scale[2];
+  const int32_t *idx;           // [Hkv][total_rows]
+  const int32_t *block_table;   // [n_seq][max_pages]
+  int max_pages, page_shift, n_pages;
+  int Hkv, total_rows, n_seq;
+  int cu[FKV_MAX_SEQS + 1];
+  int cnt_off[FKV_MAX_SEQS + 1];
+  int blk[FKV_MAX_SEQS + 1];    // prefix sums of the sequences' scale blocks
+};
+hipError_t launch_gather_quant(const QuantGatherArgs &a, int block, hipStream_t s);
+
+// ---- new tokens into a paged cache --------------------------------------------------------
+struct AppendArgs {
+  const uint16_t *q, *k, *v;    // [total][heads][d] bf16 at the strides below (elements per token); q may be nullptr
+  uint16_t *q_out;
+  int64_t q_stride, k_stride, v_stride, q_out_stride;
+  const int32_t *positions;     // [total]; with pairs > 0
+  uint64_t freq[kHeadDim / 2];  // turns per position of each pair, in units of 2^-64
+  int pairs, interleaved;       // pairs = 0: nothing is turned
+  int Hq, Hkv, n_seq, total;
+  int start[FKV_MAX_SEQS];      // tokens cached before
+  int off[FKV_MAX_SEQS + 1];    // prefix sums of the new tokens
+  const int32_t *block_table;
+  int max_pages, page_shift, n_pages;
+  uint16_t *k_pages, *v_pages;  // bf16 pools [n_pages][page_size][Hkv][d], or
+  uint8_t *k_codes, *v_codes;   // pools in 8 bits, as above
+  float *k_scale, *v_scale;
+  int blk[FKV_MAX_SEQS + 1];    // prefix sums of the scale blocks that each sequence's new tokens lie in
+};
+hipError_t launch_append(const AppendArgs &a, hipStream_t s);
+hipError_t launch_append_quant(const AppendArgs &a, int block, hipStream_t s);
 int gather_blocks_per_head(const GatherJob &j);
 hipError_t launch_gather(const GatherArgs &a, int n_blocks, hipStream_t s);
 

@@ -33,9 +33,14 @@ struct Api {
   decltype(&fkv_decode_attention_paged) decode_attention_paged;
   decltype(&fkv_window_output) window_output;
   decltype(&fkv_score_window_output) score_window_output;
+  decltype(&fkv_append_kv_paged) append_kv_paged;
+  decltype(&fkv_append_kv_paged_quant) append_kv_paged_quant;
+  decltype(&fkv_gather_kv_paged_quant) gather_kv_paged_quant;
+  decltype(&fkv_compress_kv_paged_quant) compress_kv_paged_quant;
+  decltype(&fkv_decode_attention_paged_quant) decode_attention_paged_quant;
 } api;
 
-PyTypeObject *shape_type = nullptr;
+PyTypeObject *shape_type = nullptr, *rope_type = nullptr;
 PyObject *error_type = nullptr;
 PyObject *key_k_out, *key_v_out, *key_idx_kv, *key_x_out, *key_idx_tsp;
 
@@ -71,12 +76,13 @@ struct Call {
   }
 };
 
-enum Kind { kAny, kBf16, kF32, kI32 };
+enum Kind { kAny, kBf16, kF32, kI32, kE4m3 };
 bool kind_ok(Kind kind, at::ScalarType t) {
   switch (kind) {
     case kBf16: return t == at::kBFloat16 || t == at::kShort || t == at::kUInt16;
     case kF32: return t == at::kFloat;
     case kI32: return t == at::kInt;
+    case kE4m3: return t == at::kFloat8_e4m3fn || t == at::kByte;
     default: return true;
   }
 }
@@ -408,10 +414,156 @@ PyObject *score_window_output(PyObject *const *a) {
   return Py_BuildValue("(NNN)", wrap(sg), wrap_or_none(st), wrap(out));
 }
 
-// bind(shape type, error type, {name: address}): the library the calls go to.
+// Pools of a cache in 8 bits, [n_pages][Hkv][page_size][d] codes and [n_pages][Hkv][page_size / scale_block] scales, and their block table.
+struct QuantPages {
+  fkv_quant_pages p{};
+  bool read(const Call &c, PyObject *ok, PyObject *ov, PyObject *osk, PyObject *osv, PyObject *ot, bool has_v) {
+    const at::Tensor *k = tensor(c, ok, kE4m3, 0), *sk = tensor(c, osk, kF32, 0), *table = tensor(c, ot, kI32, 0);
+    if (!k || !sk || !table || k->dim() != 4 || k->size(1) != c.hkv || k->size(3) != c.d || sk->dim() != 3 || sk->size(0) != k->size(0) ||
+        sk->size(1) != c.hkv || sk->size(2) < 1 || k->size(2) % sk->size(2) != 0 || k->size(2) > INT32_MAX || table->dim() != 2 ||
+        table->size(0) != c.n_seq || table->size(1) > INT32_MAX)
+      return false;
+    if (has_v) {
+      const at::Tensor *v = tensor(c, ov, kE4m3, 0), *sv = tensor(c, osv, kF32, 0);
+      if (!v || !sv || v->sizes() != k->sizes() || sv->sizes() != sk->sizes()) return false;
+      p.v_pages = v->data_ptr();
+      p.v_scale = f32(*sv);
+    } else if (ov != Py_None || osv != Py_None) {
+      return false;
+    }
+    p.k_pages = k->data_ptr();
+    p.k_scale = f32(*sk);
+    p.block_table = i32(*table);
+    p.max_pages_per_seq = (int32_t)table->size(1);
+    p.page_size = (int32_t)k->size(2);
+    p.scale_block = (int32_t)(k->size(2) / sk->size(2));
+    p.n_pages = k->size(0);
+    return true;
+  }
+};
+
+// [tokens][heads][d] rows, heads side by side, tokens at a stride of their own (0: one token or none).
+bool token_rows(const Call &c, PyObject *o, int64_t tokens, int64_t heads, void **ptr, int64_t *stride) {
+  if (!THPVariable_CheckExact(o)) return false;
+  const at::Tensor &t = THPVariable_Unpack(o);
+  if (!t.is_cuda() || t.get_device() != c.dev || t.layout() != at::kStrided || !kind_ok(kBf16, t.scalar_type()) || t.dim() != 3 ||
+      t.size(0) != tokens || t.size(1) != heads || t.size(2) != c.d)
+    return false;
+  if (tokens > 0 && (t.stride(2) != 1 || (heads > 1 && t.stride(1) != c.d))) return false;
+  *ptr = tokens > 0 ? t.data_ptr() : nullptr;
+  *stride = tokens > 1 ? t.stride(0) : 0;
+  return tokens <= 1 || *stride >= heads * c.d;
+}
+
+// (ctx, dev, shape, k, v, n_cached, n_new, block_table, k_pages, v_pages, k_scale, v_scale, rope, positions, q, q_out), in 8 bits with
+// k_scale; what the wrapper returns comes in a tuple, since None may be it
+PyObject *append_kv_paged(PyObject *const *a) {
+  Call c;
+  Counts cached, fresh;
+  if (!c.open(a) || !cached.read(c, a[5]) || !fresh.read(c, a[6])) return none();
+  const bool quant = a[10] != Py_None, has_q = a[14] != Py_None, has_rope = a[12] != Py_None;
+  fkv_new_tokens t{};
+  void *k, *v, *q, *qo;
+  if (!token_rows(c, a[3], fresh.sum, c.hkv, &k, &t.k_stride) || !token_rows(c, a[4], fresh.sum, c.hkv, &v, &t.v_stride)) return none();
+  t.k = k, t.v = v;
+  const fkv_rope *rope = nullptr;
+  if (has_rope) {
+    Py_buffer buf;
+    if (rope_type == nullptr || !PyObject_TypeCheck(a[12], rope_type)) return none();
+    if (PyObject_GetBuffer(a[12], &buf, PyBUF_SIMPLE) != 0) { PyErr_Clear(); return none(); }
+    rope = buf.len >= (Py_ssize_t)sizeof(fkv_rope) ? static_cast<const fkv_rope *>(buf.buf) : nullptr;
+    PyBuffer_Release(&buf);
+    const at::Tensor *pos = tensor(c, a[13], kI32, fresh.sum);
+    if (rope == nullptr || pos == nullptr) return none();
+    t.positions = i32(*pos);
+  }
+  if (!has_rope && has_q) return none();
+  if (!has_q && a[15] != Py_None) return none();
+  at::Tensor out;
+  if (has_q) {
+    if (!token_rows(c, a[14], fresh.sum, c.hq, &q, &t.q_stride)) return none();
+    if (a[15] == Py_None) {
+      out = at::empty({fresh.sum, c.hq, c.d}, THPVariable_Unpack(a[14]).options());
+      qo = out.data_ptr();
+    } else if (token_rows(c, a[15], fresh.sum, c.hq, &qo, &t.q_out_stride)) {
+      out = THPVariable_Unpack(a[15]);
+    } else {
+      return none();
+    }
+    t.q = q, t.q_out = qo;
+  }
+  t.n_cached = cached.v;
+  t.n_new = fresh.v;
+  bool ok;
+  if (quant) {
+    QuantPages p;
+    if (!p.read(c, a[8], a[9], a[10], a[11], a[7], true)) return none();
+    ok = call("fkv_append_kv_paged_quant", [&] { return api.append_kv_paged_quant(c.ctx, c.shape, rope, &t, &p.p, c.stream); });
+  } else {
+    Pages p;
+    if (a[11] != Py_None || !p.read(c, a[8], a[9], a[7])) return none();
+    ok = call("fkv_append_kv_paged", [&] {
+      return api.append_kv_paged(c.ctx, c.shape, rope, &t, i32(*p.table), (int32_t)p.table->size(1), (int32_t)p.k->size(1), p.k->size(0),
+                                 p.k->data_ptr(), p.v->data_ptr(), c.stream);
+    });
+  }
+  if (!ok) return none();
+  return Py_BuildValue("(N)", wrap_or_none(out));
+}
+
+// (ctx, dev, shape, k, v, idx, budget, block_table, k_pages, v_pages, k_scale, v_scale): True if done
+PyObject *gather_kv_paged_quant(PyObject *const *a) {
+  Call c;
+  Counts n;
+  QuantPages p;
+  const bool has_v = a[4] != Py_None;
+  if (!c.open(a) || !n.read(c, a[6]) || !p.read(c, a[8], a[9], a[10], a[11], a[7], has_v)) return none();
+  const at::Tensor *k = tensor(c, a[3], kBf16, c.kv), *v = has_v ? tensor(c, a[4], kBf16, c.kv) : nullptr;
+  const at::Tensor *idx = tensor(c, a[5], kI32, c.hkv * n.sum);
+  if (!k || !idx || (has_v && !v)) return none();
+  if (!call("fkv_gather_kv_paged_quant", [&] {
+        return api.gather_kv_paged_quant(c.ctx, c.shape, k->data_ptr(), has_v ? v->data_ptr() : nullptr, i32(*idx), n.v, &p.p, c.stream);
+      }))
+    return none();
+  Py_RETURN_TRUE;
+}
+
+// (ctx, dev, shape, q_win, k, v, budget, block_table, k_pages, v_pages, k_scale, v_scale, idx_kv)
+PyObject *compress_kv_paged_quant(PyObject *const *a) {
+  Call c;
+  Counts n;
+  QuantPages p;
+  if (!c.open(a) || !n.read(c, a[6]) || !p.read(c, a[8], a[9], a[10], a[11], a[7], true)) return none();
+  const at::Tensor *q = tensor(c, a[3], kBf16, c.q_win), *k = tensor(c, a[4], kBf16, c.kv), *v = tensor(c, a[5], kBf16, c.kv);
+  at::Tensor idx;
+  if (!q || !k || !v || !output(c, a[12], kI32, c.hkv * n.sum, {c.hkv, n.sum}, at::kInt, idx)) return none();
+  if (!call("fkv_compress_kv_paged_quant", [&] {
+        return api.compress_kv_paged_quant(c.ctx, c.shape, q->data_ptr(), k->data_ptr(), v->data_ptr(), n.v, &p.p, i32(idx), c.stream);
+      }))
+    return none();
+  return wrap(idx);
+}
+
+// (ctx, dev, shape, q, k_pages, v_pages, k_scale, v_scale, block_table, n_per_seq, out)
+PyObject *decode_attention_paged_quant(PyObject *const *a) {
+  Call c;
+  Counts n;
+  QuantPages p;
+  if (!c.open(a) || !n.read(c, a[9]) || !p.read(c, a[4], a[5], a[6], a[7], a[8], true)) return none();
+  const at::Tensor *q = tensor(c, a[3], kBf16, c.q_dec);
+  at::Tensor out;
+  if (!q || !output(c, a[10], kF32, c.q_dec, {c.n_seq, c.hq, c.d}, at::kFloat, out)) return none();
+  if (!call("fkv_decode_attention_paged_quant", [&] {
+        return api.decode_attention_paged_quant(c.ctx, c.shape, q->data_ptr(), &p.p, n.v, f32(out), c.stream);
+      }))
+    return none();
+  return wrap(out);
+}
+
+// bind(shape type, error type, {name: address}[, rope type]): the library the calls go to.
 PyObject *bind(PyObject *, PyObject *args) {
-  PyObject *type, *error, *addresses;
-  if (!PyArg_ParseTuple(args, "O!O!O!", &PyType_Type, &type, &PyType_Type, &error, &PyDict_Type, &addresses)) return nullptr;
+  PyObject *type, *error, *addresses, *rope = nullptr;
+  if (!PyArg_ParseTuple(args, "O!O!O!|O!", &PyType_Type, &type, &PyType_Type, &error, &PyDict_Type, &addresses, &PyType_Type, &rope)) return nullptr;
   bool ok = true;
   auto get = [&](auto &slot, const char *name) {
     PyObject *o = PyDict_GetItemString(addresses, name);
@@ -431,6 +583,11 @@ PyObject *bind(PyObject *, PyObject *args) {
   get(api.decode_attention_paged, "fkv_decode_attention_paged");
   get(api.window_output, "fkv_window_output");
   get(api.score_window_output, "fkv_score_window_output");
+  get(api.append_kv_paged, "fkv_append_kv_paged");
+  get(api.append_kv_paged_quant, "fkv_append_kv_paged_quant");
+  get(api.gather_kv_paged_quant, "fkv_gather_kv_paged_quant");
+  get(api.compress_kv_paged_quant, "fkv_compress_kv_paged_quant");
+  get(api.decode_attention_paged_quant, "fkv_decode_attention_paged_quant");
   if (!ok) {
     shape_type = nullptr;
     if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "bind: a function address is missing");
@@ -438,6 +595,10 @@ PyObject *bind(PyObject *, PyObject *args) {
   }
   Py_INCREF(type);
   Py_INCREF(error);
+  if (rope != nullptr) {
+    Py_INCREF(rope);
+    rope_type = reinterpret_cast<PyTypeObject *>(rope);
+  }
   error_type = error;
   shape_type = reinterpret_cast<PyTypeObject *>(type);
   Py_RETURN_NONE;
@@ -459,6 +620,10 @@ PyMethodDef methods[] = {
     FKV_METHOD("decode_attention_paged", decode_attention_paged, 9),
     FKV_METHOD("window_output", window_output, 7),
     FKV_METHOD("score_window_output", score_window_output, 10),
+    FKV_METHOD("append_kv_paged", append_kv_paged, 16),
+    FKV_METHOD("gather_kv_paged_quant", gather_kv_paged_quant, 12),
+    FKV_METHOD("compress_kv_paged_quant", compress_kv_paged_quant, 13),
+    FKV_METHOD("decode_attention_paged_quant", decode_attention_paged_quant, 11),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
