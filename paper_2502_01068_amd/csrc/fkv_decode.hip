@@ -34,19 +34,10 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "fkv_dpp.h"
-#include "fkv_internal.h"
+#include "fkv_decode_common.h"
 
 
 namespace fkv {
-
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(4))) float floatx4;
-
-constexpr int kDecTile = 32;                  // tokens a wave works on at a time
-constexpr float kDecNegBig = -1.0e30f;
-
-__device__ __forceinline__ float dec_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // The K tile's operands: waits until at most the 8 youngest loads (the V tile's) are outstanding, reads and waits for
 // the reads, so that the tile may be overwritten.  One asm block: for an ordinary LDS read the compiler would
@@ -85,41 +76,10 @@ __device__ __forceinline__ void read_queries(bf16x8 (&qb)[4], uint32_t addr, boo
   for (int s = 0; s < 4; ++s) qb[s] = __builtin_bit_cast(bf16x8, live ? r[s] : u32x4{0u, 0u, 0u, 0u});
 }
 
-// The sum a row is divided by.  Zero: no token has a finite logit and the softmax no value; NaN then, and not what the
-// kept-up pieces of the probabilities (see k_decode) divided by zero would give.
-__device__ __forceinline__ float row_sum(float l) { return l > 0.f ? l : __uint_as_float(0x7FC00000u); }
-
-__device__ __forceinline__ void agent_store2(float *p, float x, float y) {
-  const float2 v = make_float2(x, y);
-  unsigned long long bits;
-  __builtin_memcpy(&bits, &v, sizeof bits);
-  __hip_atomic_store(reinterpret_cast<unsigned long long *>(p), bits, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 agent_load2(const float *p) {
-  const unsigned long long bits =
-      __hip_atomic_load(reinterpret_cast<const unsigned long long *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  float2 v;
-  __builtin_memcpy(&v, &bits, sizeof v);
-  return v;
-}
-
-// The work of a launch is a line of 32-token tiles, row after row (a row = one KV head of one sequence); block i
-// of N takes tiles [i T / N, (i + 1) T / N).  A row that lies inside one block is finished there; the pieces of a row
-// that is cut go to partial slots, at most two per block (2 i: a piece that does not begin its row, 2 i + 1: one that does).
-// T < 2^30; the products of these bounds are not, so they are formed from quotient and remainder.
-__device__ __forceinline__ uint32_t share_at(uint32_t len, uint32_t part, uint32_t parts) {  // len * part / parts
-  const uint32_t per = len / parts, rem = len - per * parts;
-  return part * per + part * rem / parts;
-}
-__device__ __forceinline__ int dec_block_of(uint64_t tile, uint64_t tiles, uint64_t n_blocks) {
-  return (int)(((tile + 1) * n_blocks - 1) / tiles);
-}
-
 // kAligned: every row of sequence b is cut into a.piece0[b + 1] - a.piece0[b] equal pieces, one per block (KV heads
 // fastest), instead of equal shares of the line of tiles.  kPauses: the K requests of a tile go out in pairs, see launch_decode.
 template <bool kPaged, bool kAligned, bool kPauses, int kWaves>
 __global__ __launch_bounds__(kWaves * 64, 2) void k_decode(DecodeArgs a) {
-  constexpr int kThr = kWaves * 64;
   constexpr int kTileBytes = kDecTile * kHeadDim * 2;
   __shared__ __attribute__((aligned(16))) uint8_t k_lds[kWaves][kTileBytes];
   __shared__ __attribute__((aligned(16))) float o_lds[kWaves][kMaxReal][kHeadDim];
@@ -356,94 +316,20 @@ __global__ __launch_bounds__(kWaves * 64, 2) void k_decode(DecodeArgs a) {
       if (q == 0) { m_lds[wave][c] = m; l_lds[wave][c] = l; }
     }
     __syncthreads();
-    const bool whole = tile0 == 0 && tile1 == row_tiles;  // this block has the entire row
-    float *part = a.part + (2 * (size_t)blockIdx.x + (!kAligned && tile0 == 0 ? 1 : 0)) * kDecodeSlotFloats;
-    float *out = a.out + ((size_t)b * a.Hq + (size_t)kvh * G) * kHeadDim;
-    for (int e = tid; e < G * (kHeadDim / 2); e += kThr) {
-      const int h = e >> 6, d = (e & 63) * 2;
-      float M = m_lds[0][h];
-#pragma unroll
-      for (int w = 1; w < kWaves; ++w) M = fmaxf(M, m_lds[w][h]);
-      float L = 0.f, x = 0.f, y = 0.f;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const float f = dec_exp2(m_lds[w][h] - M);
-        const float2 ov = *reinterpret_cast<const float2 *>(&o_lds[w][h][d]);
-        L += f * l_lds[w][h];
-        x += f * ov.x;
-        y += f * ov.y;
-      }
-      if (whole) {
-        const float sum = row_sum(L);
-        *reinterpret_cast<float2 *>(out + h * kHeadDim + d) = make_float2(x / sum, y / sum);
-      } else {
-        agent_store2(part + h * kHeadDim + d, x, y);
-        if (d == 0) agent_store2(part + kMaxReal * kHeadDim + 2 * h, M, L);
-      }
-    }
+    finish_piece<kAligned, kWaves>(a, &o_lds[0][0][0], kMaxReal * kHeadDim, m_lds, l_lds, &last_lds, DecPiece{b, kvh, tile0, tile1, row_tiles, row_at, piece_blk0, n_piece});
     at = row_at + tile1;
-    if (whole) {
-      if (kAligned) return;
-      __syncthreads();  // the next piece reuses the tables
-      continue;
-    }
-
-    // ---- count this piece; the last one of the row folds them
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    const int blk0 = kAligned ? piece_blk0 : dec_block_of(row_at, a.tiles, gridDim.x);
-    const int n_split = kAligned ? n_piece : dec_block_of(row_at + row_tiles - 1, a.tiles, gridDim.x) - blk0 + 1;
-    unsigned *count = a.count + b * kMaxKvHeads + kvh;
-    if (tid == 0) {
-      const unsigned old = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      last_lds = old + 1u == (unsigned)n_split ? 1u : 0u;
-    }
-    __syncthreads();
-    if (last_lds != 0u) {
-      if (tid == 0) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // ready for the next launch
-      // equal shares: piece p of the row lies in block blk0 + p; only the first one begins the row
-      const float *src = a.part + 2 * (size_t)blk0 * kDecodeSlotFloats;
-      auto piece = [&](int p) { return src + (size_t)(kAligned ? 2 * p * a.Hkv : p == 0 ? 1 : 2 * p) * kDecodeSlotFloats; };
-      constexpr int kBatch = 16;  // partial rows in flight per lane
-      for (int h = wave; h < G; h += kWaves) {  // one wave per head, two columns per lane
-        const float2 ml = agent_load2(piece(min(lane, n_split - 1)) + kMaxReal * kHeadDim + 2 * h);
-        float2 v[kBatch];
-        auto request = [&](int s0) {
-#pragma unroll
-          for (int i = 0; i < kBatch; ++i) v[i] = agent_load2(piece(min(s0 + i, n_split - 1)) + h * kHeadDim + 2 * lane);
-        };
-        request(0);
-        // the pieces' weights, a lane each
-        const float mp = lane < n_split ? ml.x : kDecNegBig;
-        const float f = dec_exp2(mp - wave_fmax(mp));
-        const float L = row_sum(wave_fsum(lane < n_split ? ml.y * f : 0.f));
-        const int weight = __float_as_int(lane < n_split ? f / L : 0.f);
-        float x = 0.f, y = 0.f;
-        for (int s0 = 0; s0 < n_split; s0 += kBatch) {
-          if (s0 > 0) request(s0);
-#pragma unroll
-          for (int i = 0; i < kBatch; ++i) {  // past the last piece nothing is added: 0 times an infinite sum would be NaN
-            const float w = __int_as_float(__builtin_amdgcn_readlane(weight, s0 + i));
-            x += s0 + i < n_split ? v[i].x * w : 0.f;
-            y += s0 + i < n_split ? v[i].y * w : 0.f;
-          }
-        }
-        *reinterpret_cast<float2 *>(out + h * kHeadDim + 2 * lane) = make_float2(x, y);
-      }
-    }
     if (kAligned) return;
     __syncthreads();
   }
 }
 
-// Tiles of every sequence (a.tile0, a.tiles), the blocks to spread them over, and the launch.
-hipError_t launch_decode(DecodeArgs &a, int n_cu, hipStream_t s) {
-  constexpr int kWaves = 4;
-  const dim3 block(kWaves * 64);
+// Tiles of every sequence (a.tile0, a.tiles; a sequence without tokens has one, nothing of which counts), and the blocks to spread them over.
+DecodePlan plan_decode(DecodeArgs &a, int n_cu) {
+  constexpr int kWaves = kDecWaves;
   int64_t tiles = 0, longest = 1;
   a.tile0[0] = 0;
   for (int b = 0; b < a.n_seq; ++b) {
-    const int64_t t = (a.off[b + 1] - a.off[b] + kDecTile - 1) / kDecTile;
+    const int64_t t = std::max((a.off[b + 1] - a.off[b] + kDecTile - 1) / kDecTile, 1);
     tiles += t;
     longest = std::max(longest, t);
     a.tile0[b + 1] = (int)tiles;
@@ -456,13 +342,6 @@ hipError_t launch_decode(DecodeArgs &a, int n_cu, hipStream_t s) {
   //   costs more than it saves (160 rows of 250 tokens 7.4 against 13.9).
   //   Pieces: few rows, or few tiles per CU (128 rows of 1000 tokens 14.2 against 17 us; of 5000, 63 against 55.7).
   constexpr int kWholeTiles = 12;
-  // Pauses between K requests, for a token-major cache and 40 tiles per block or more.  The heads' blocks read 256 bytes each of the
-  // same 2 KiB; all 8 requests of a tile at once (one addition each; a 64-bit product each used to space them) disturb that.
-  // With pauses, without, with the products: 32 sequences of 3600-4000 tokens 79.1, 80.3, 79.2 us, 32 of 2048 43.6, 44.5, 43.9, 12 of
-  // 7000-8000 65.7, 66.5, 66.2, one of 120000 79.2, 80.3, 80.1.  Fewer tiles and a compact cache are faster without: one sequence of
-  // 32768 (32 tiles per block) 25.9, 25.6, 26.7; 48 of 500-1000 31.8, 31.3, 33.6; compact 32 of 3600-4000 76.5, 76.0, 77.1.
-  constexpr int kPausesTiles = 40;
-  auto pauses = [&](dim3 grid) { return a.tok_stride > kHeadDim && a.tiles >= (int64_t)kPausesTiles * grid.x; };
   const int rows = a.n_seq * a.Hkv;
   const int per_cu = (rows + n_cu - 1) / n_cu;
   const bool even = 10 * rows >= 9 * per_cu * n_cu && 2 * longest * a.n_seq <= 3 * tiles;
@@ -475,14 +354,7 @@ hipError_t launch_decode(DecodeArgs &a, int n_cu, hipStream_t s) {
       int64_t n = even || t <= kWholeTiles ? 1 : std::min<int64_t>((2 * t + share) / (2 * share), kDecodeMaxSplits);
       a.piece0[b + 1] = a.piece0[b] + (int)std::max<int64_t>(n, 1);
     }
-    const dim3 grid((unsigned)(a.piece0[a.n_seq] * a.Hkv));
-    if (a.block_table)
-      hipLaunchKernelGGL((k_decode<true, true, false, kWaves>), grid, block, 0, s, a);
-    else if (pauses(grid))
-      hipLaunchKernelGGL((k_decode<false, true, true, kWaves>), grid, block, 0, s, a);
-    else
-      hipLaunchKernelGGL((k_decode<false, true, false, kWaves>), grid, block, 0, s, a);
-    return hipGetLastError();
+    return {a.piece0[a.n_seq] * a.Hkv, true};
   }
   // Equal shares: one block per CU; two where a block goes through several short rows, as each starts with the latency
   // of its first loads, which the other block then covers.
@@ -490,10 +362,32 @@ hipError_t launch_decode(DecodeArgs &a, int n_cu, hipStream_t s) {
   int64_t blocks = std::min<int64_t>(std::min(shares * n_cu, kDecodeMaxBlocks), ((int64_t)a.tiles + kWaves - 1) / kWaves);
   // a row is cut into at most kDecodeMaxSplits pieces: the fold keeps a weight for each
   blocks = std::max<int64_t>(1, std::min<int64_t>(blocks, (int64_t)a.tiles * (kDecodeMaxSplits - 2) / longest));
-  const dim3 grid((unsigned)blocks);
+  return {(int)blocks, false};
+}
+
+hipError_t launch_decode(DecodeArgs &a, int n_cu, hipStream_t s) {
+  constexpr int kWaves = kDecWaves;
+  const DecodePlan plan = plan_decode(a, n_cu);
+  const dim3 grid(plan.blocks), block(kWaves * 64);
+  // Pauses between K requests, for a token-major cache and 40 tiles per block or more.  The heads' blocks read 256 bytes each of the
+  // same 2 KiB; all 8 requests of a tile at once (one addition each; a 64-bit product each used to space them) disturb that.
+  // With pauses, without, with the products: 32 sequences of 3600-4000 tokens 79.1, 80.3, 79.2 us, 32 of 2048 43.6, 44.5, 43.9, 12 of
+  // 7000-8000 65.7, 66.5, 66.2, one of 120000 79.2, 80.3, 80.1.  Fewer tiles and a compact cache are faster without: one sequence of
+  // 32768 (32 tiles per block) 25.9, 25.6, 26.7; 48 of 500-1000 31.8, 31.3, 33.6; compact 32 of 3600-4000 76.5, 76.0, 77.1.
+  constexpr int kPausesTiles = 40;
+  const bool pauses = a.tok_stride > kHeadDim && a.tiles >= (int64_t)kPausesTiles * plan.blocks;
+  if (plan.aligned) {
+    if (a.block_table)
+      hipLaunchKernelGGL((k_decode<true, true, false, kWaves>), grid, block, 0, s, a);
+    else if (pauses)
+      hipLaunchKernelGGL((k_decode<false, true, true, kWaves>), grid, block, 0, s, a);
+    else
+      hipLaunchKernelGGL((k_decode<false, true, false, kWaves>), grid, block, 0, s, a);
+    return hipGetLastError();
+  }
   if (a.block_table)
     hipLaunchKernelGGL((k_decode<true, false, false, kWaves>), grid, block, 0, s, a);
-  else if (pauses(grid))
+  else if (pauses)
     hipLaunchKernelGGL((k_decode<false, false, true, kWaves>), grid, block, 0, s, a);
   else
     hipLaunchKernelGGL((k_decode<false, false, false, kWaves>), grid, block, 0, s, a);
