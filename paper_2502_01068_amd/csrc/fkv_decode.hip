@@ -324,8 +324,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void k_decode(DecodeArgs a) {
 }
 
 // Tiles of every sequence (a.tile0, a.tiles; a sequence without tokens has one, nothing of which counts), and the blocks to spread them over.
-DecodePlan plan_decode(DecodeArgs &a, int n_cu) {
-  constexpr int kWaves = kDecWaves;
+DecodePlan plan_decode(DecodeArgs &a, int n_cu, int waves, bool whole_rounds) {
   int64_t tiles = 0, longest = 1;
   a.tile0[0] = 0;
   for (int b = 0; b < a.n_seq; ++b) {
@@ -341,25 +340,36 @@ DecodePlan plan_decode(DecodeArgs &a, int n_cu) {
   //   against 56 us, of 1280-2560 45.6 against 48; but 320 rows 54 against 47.7); rows of up to 12 tiles, where a fold
   //   costs more than it saves (160 rows of 250 tokens 7.4 against 13.9).
   //   Pieces: few rows, or few tiles per CU (128 rows of 1000 tokens 14.2 against 17 us; of 5000, 63 against 55.7).
-  constexpr int kWholeTiles = 12;
+  const int whole_tiles = whole_rounds ? 16 : 12;  // in 8 bits (a row of 512 tokens 7.8 us in two pieces, 7.2 whole; of 768 7.9, 8.5)
   const int rows = a.n_seq * a.Hkv;
   const int per_cu = (rows + n_cu - 1) / n_cu;
   const bool even = 10 * rows >= 9 * per_cu * n_cu && 2 * longest * a.n_seq <= 3 * tiles;
   const bool pieces = 4 * rows <= n_cu || (rows <= n_cu && a.tiles <= (int64_t)48 * n_cu);  // <= 1.5 n_cu of them
-  if (even || pieces || longest <= kWholeTiles) {
-    const int64_t share = std::max<int64_t>(kWaves, ((int64_t)a.tiles + n_cu - 1) / n_cu);
-    a.piece0[0] = 0;
-    for (int b = 0; b < a.n_seq; ++b) {
-      const int64_t t = a.tile0[b + 1] - a.tile0[b];
-      int64_t n = even || t <= kWholeTiles ? 1 : std::min<int64_t>((2 * t + share) / (2 * share), kDecodeMaxSplits);
-      a.piece0[b + 1] = a.piece0[b] + (int)std::max<int64_t>(n, 1);
+  if (even || pieces || longest <= whole_tiles) {
+    int64_t share = std::max<int64_t>(waves, ((int64_t)a.tiles + n_cu - 1) / n_cu);
+    // In 8 bits the fold weighs more beside the tiles: a block's waves all get as many, and two each rather than more than half of the blocks
+    // (8192 tokens in 256 pieces 11.4 us, in 128 10.4; 4096 in 128 8.8, in 64 9.4; 16384 in 256 13.9, in 128 14.4).
+    if (whole_rounds) {
+      share = (share + waves - 1) / waves * waves;
+      if (share == waves && 2 * (int64_t)a.tiles > share * n_cu) share *= 2;
+    }
+    while (true) {
+      a.piece0[0] = 0;
+      for (int b = 0; b < a.n_seq; ++b) {
+        const int64_t t = a.tile0[b + 1] - a.tile0[b];
+        int64_t n = even || t <= whole_tiles ? 1 : std::min<int64_t>((2 * t + share) / (2 * share), kDecodeMaxSplits);
+        a.piece0[b + 1] = a.piece0[b] + (int)std::max<int64_t>(n, 1);
+      }
+      // nor a second round of few blocks (160 rows of 768 tokens in 320 pieces 16.9, whole 11.2)
+      if (!whole_rounds || a.piece0[a.n_seq] * a.Hkv <= n_cu || a.piece0[a.n_seq] == a.n_seq) break;
+      share += waves;
     }
     return {a.piece0[a.n_seq] * a.Hkv, true};
   }
   // Equal shares: one block per CU; two where a block goes through several short rows, as each starts with the latency
   // of its first loads, which the other block then covers.
   const int shares = rows > n_cu && a.tiles <= (int64_t)rows * 16 ? 2 : 1;
-  int64_t blocks = std::min<int64_t>(std::min(shares * n_cu, kDecodeMaxBlocks), ((int64_t)a.tiles + kWaves - 1) / kWaves);
+  int64_t blocks = std::min<int64_t>(std::min(shares * n_cu, kDecodeMaxBlocks), ((int64_t)a.tiles + waves - 1) / waves);
   // a row is cut into at most kDecodeMaxSplits pieces: the fold keeps a weight for each
   blocks = std::max<int64_t>(1, std::min<int64_t>(blocks, (int64_t)a.tiles * (kDecodeMaxSplits - 2) / longest));
   return {(int)blocks, false};
@@ -367,7 +377,7 @@ DecodePlan plan_decode(DecodeArgs &a, int n_cu) {
 
 hipError_t launch_decode(DecodeArgs &a, int n_cu, hipStream_t s) {
   constexpr int kWaves = kDecWaves;
-  const DecodePlan plan = plan_decode(a, n_cu);
+  const DecodePlan plan = plan_decode(a, n_cu, kWaves, false);
   const dim3 grid(plan.blocks), block(kWaves * 64);
   // Pauses between K requests, for a token-major cache and 40 tiles per block or more.  The heads' blocks read 256 bytes each of the
   // same 2 KiB; all 8 requests of a tile at once (one addition each; a 64-bit product each used to space them) disturb that.

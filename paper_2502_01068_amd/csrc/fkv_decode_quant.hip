@@ -342,12 +342,19 @@ __global__ __launch_bounds__(kWaves * 64, 2) void k_decode_quant(DecodeQuantArgs
 }
 
 hipError_t launch_decode_quant(DecodeQuantArgs &a, int n_cu, hipStream_t s) {
-  const DecodePlan plan = plan_decode(a.d, n_cu);
-  const dim3 grid(plan.blocks), block(kDecWaves * 64);
-  if (plan.aligned)
-    hipLaunchKernelGGL((k_decode_quant<true, kDecWaves>), grid, block, 0, s, a);
-  else
-    hipLaunchKernelGGL((k_decode_quant<false, kDecWaves>), grid, block, 0, s, a);
+  // Blocks of 8 waves, one to a CU (149 KB of LDS), or where there are more rows than CUs two of 4 waves each, so that one block's start is
+  // covered by the other.  us, 8 waves and 4: 256 rows of 2048-2560 tokens 29.3, 30.6; one sequence of 131072 (8 rows) 47.1, 49.0; 128 rows of
+  // 1000 12.5, 12.3; but 512 rows of 2000 50.3, 45.4; of 200 13.5, 9.9; 384 rows of 500-1000 25.2, 23.0; 264 of 600-1200 21.1, 17.5.
+  const bool wide = a.d.n_seq * a.d.Hkv <= n_cu;
+  const DecodePlan plan = wide ? plan_decode(a.d, n_cu, 8, true) : plan_decode(a.d, 2 * n_cu, 4, true);
+  auto launch = [&](auto aligned_t, auto waves_t) {
+    constexpr int kWaves = decltype(waves_t)::value;
+    hipLaunchKernelGGL((k_decode_quant<decltype(aligned_t)::value, kWaves>), dim3(plan.blocks), dim3(kWaves * 64), 0, s, a);
+  };
+  using four = std::integral_constant<int, 4>;
+  using eight = std::integral_constant<int, 8>;
+  if (plan.aligned) wide ? launch(std::true_type{}, eight{}) : launch(std::true_type{}, four{});
+  else wide ? launch(std::false_type{}, eight{}) : launch(std::false_type{}, four{});
   return hipGetLastError();
 }
 

@@ -222,12 +222,12 @@ struct DecodeArgs {
   const int32_t *block_table;
   int max_pages, page_shift, n_pages;
 };
-constexpr int kDecWaves = 4;  // of a block
+constexpr int kDecWaves = 4;  // of a block, over a bf16 cache
 struct DecodePlan {
   int blocks;
   bool aligned;  // every row is whole or cut into equal pieces (piece0), one per block; else the line of all tiles is cut into equal shares
 };
-DecodePlan plan_decode(DecodeArgs &a, int n_cu);
+DecodePlan plan_decode(DecodeArgs &a, int n_cu, int waves, bool whole_rounds);
 hipError_t launch_decode(DecodeArgs &a, int n_cu, hipStream_t s);
 
 // The same over a cache held in 8 bits: page pools [n_pages][Hkv][page_size][d] of e4m3 codes, a scale for every 1 << block_shift tokens
