@@ -42,7 +42,7 @@ WsLayout ws_layout(int64_t max_tokens, int32_t max_seqs) {
   w.sel_long = off;     off += align_up((size_t)kLongMaxInst * kLongStateWords * sizeof(uint32_t));
   w.sel_coop = off;     off += align_up(kCoopBoxBytes);
   w.dec_part = off;     off += align_up((size_t)2 * kDecodeMaxBlocks * kDecodeSlotFloats * sizeof(float));
-  w.dec_count = off;    off += align_up((size_t)max_seqs * kMaxKvHeads * sizeof(unsigned));
+  w.dec_count = off;    off += align_up((size_t)max_seqs * kMaxKvHeads * kDecodeCountStride * sizeof(unsigned));
   const size_t wout_slots = (size_t)kWoutBlocks + (size_t)kMaxVGroups * max_seqs;
   w.wout_o = off;       off += wout_sum_bytes(max_tokens) + align_up(wout_slots * kRowsPerGroup * kHeadDim * sizeof(float));  // the window sums first
   w.wout_ms = off;      off += align_up(wout_slots * kRowsPerGroup * sizeof(float2));
@@ -657,7 +657,7 @@ hipError_t reset_select_exchange(fkv_ctx *c) {
 
 // Pieces that have finished, per row: zero between launches, unless one was cut short or overlapped another.
 hipError_t reset_decode_counts(fkv_ctx *c) {
-  return hipMemset(c->ws + c->lay.dec_count, 0, (size_t)c->max_seqs * kMaxKvHeads * sizeof(unsigned));
+  return hipMemset(c->ws + c->lay.dec_count, 0, (size_t)c->max_seqs * kMaxKvHeads * kDecodeCountStride * sizeof(unsigned));
 }
 }  // namespace
 

@@ -123,7 +123,7 @@ __device__ __forceinline__ void finish_piece(const DecodeArgs &a, const float *o
   __syncthreads();
   const int blk0 = kAligned ? w.blk0 : dec_block_of(w.row_at, a.tiles, gridDim.x);
   const int n_split = kAligned ? w.n_piece : dec_block_of(w.row_at + w.row_tiles - 1, a.tiles, gridDim.x) - blk0 + 1;
-  unsigned *count = a.count + w.b * kMaxKvHeads + w.kvh;
+  unsigned *count = a.count + (w.b * kMaxKvHeads + w.kvh) * kDecodeCountStride;
   if (tid == 0) {
     const unsigned old = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     *last = old + 1u == (unsigned)n_split ? 1u : 0u;

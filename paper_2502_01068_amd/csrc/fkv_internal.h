@@ -203,13 +203,14 @@ hipError_t launch_select_long(const SelectArgs &a, int rows, int max_slices, hip
 // ---- decode attention over the cache ----------------------------------------------------
 constexpr int kDecodeMaxSplits = 64;    // pieces one (sequence, KV head) row is cut into
 constexpr int kDecodeMaxBlocks = 1024;  // blocks per launch, two partial slots each
+constexpr int kDecodeCountStride = 32;  // words: a row's count has a cache line of its own
 constexpr int kDecodeSlotFloats = kMaxReal * kHeadDim + 32;  // one block's partial: [G][d] weighted sums, then (max, sum) pairs; whole cache lines
 struct DecodeArgs {
   const uint16_t *q;     // [B][Hq][d]
   const uint16_t *k, *v; // element (b, g, t) at g*head_stride + (off[b] + t)*tok_stride
   float *out;            // [B][Hq][d]
   float *part;           // [2 * blocks][kDecodeSlotFloats]
-  unsigned *count;       // [B][kMaxKvHeads]: blocks that finished, zero between launches
+  unsigned *count;       // [B][kMaxKvHeads][kDecodeCountStride]: first word: blocks that finished, zero between launches
   int64_t tok_stride, head_stride;
   int Hq, Hkv, G, n_seq;
   float scale_log2e;
