@@ -11,9 +11,16 @@
 
 namespace fkv {
 
-constexpr int kAppendThreads = 256;
 constexpr int kRowLanes = 8;  // threads of a row
+constexpr int kAppendMaxThreads = (kMaxKvHeads * kMaxReal + 2 * kMaxKvHeads) * kRowLanes;  // of a token
 constexpr int kPairs = kHeadDim / 2;
+
+// A launch's arguments where the hardware finds them.  (Through an ordinary reference, an index that differs between lanes, or a choice between
+// two members, made the compiler copy all 1.6 KB to each lane's scratch memory first.)
+typedef const __attribute__((address_space(4))) AppendArgs AppendKernArgs;
+typedef const __attribute__((address_space(4))) QuantGatherArgs GatherKernArgs;
+typedef const __attribute__((address_space(4))) int *kern_ints_t;
+#define FKV_KERN_ARGS(type) (*(type *)__builtin_amdgcn_kernarg_segment_ptr())
 
 // sine and cosine of a block's tokens, a row of kPairs each
 template <int kTok>
@@ -23,7 +30,7 @@ struct TurnTable {
 
 // Fills rows 0 .. n - 1 of the table for the packed tokens token0, token0 + 1, ..; all threads of the block.
 template <int kTok>
-__device__ __forceinline__ void fill_turns(const AppendArgs &a, TurnTable<kTok> &t, int token0, int n) {
+__device__ __forceinline__ void fill_turns(AppendKernArgs &a, TurnTable<kTok> &t, int token0, int n) {
   for (int e = threadIdx.x; e < n * kPairs; e += blockDim.x) {
     const int tok = e / kPairs, i = e % kPairs;
     if (i < a.pairs) {
@@ -38,18 +45,14 @@ struct RowPart {
   int first, second;
   bool turned;
 };
-__device__ __forceinline__ RowPart row_part(const AppendArgs &a, int j, bool rotate) {
+__device__ __forceinline__ RowPart row_part(AppendKernArgs &a, int j, bool rotate) {
   const int n_turn = a.pairs / 8;
-  RowPart p{2 * j, 2 * j + 1, rotate && j < n_turn};
-  if (p.turned && !a.interleaved) {
-    p.first = j;
-    p.second = j + n_turn;
-  }
-  return p;
+  const bool turned = rotate && j < n_turn;
+  return turned && !a.interleaved ? RowPart{j, j + n_turn, true} : RowPart{2 * j, 2 * j + 1, turned};
 }
 
 // The 16 values of a thread's chunks, turned by the pairs' angles.
-__device__ __forceinline__ void turn16(const AppendArgs &a, u32x4 first, u32x4 second, const float *cs, const float *sn, float (&x)[16]) {
+__device__ __forceinline__ void turn16(AppendKernArgs &a, u32x4 first, u32x4 second, const float *cs, const float *sn, float (&x)[16]) {
   float v[16], c[8], s[8];
   unpack8(first, v);
   unpack8(second, v + 8);
@@ -70,15 +73,15 @@ __device__ __forceinline__ void turn16(const AppendArgs &a, u32x4 first, u32x4 s
   }
 }
 
-__device__ __forceinline__ int seq_at(const int *off, int n_seq, int i) {  // the sequence that entry i of a packed batch belongs to
-  int b = 0;
-  while (b + 1 < n_seq && i >= off[b + 1]) ++b;
-  return b;
+// The sequence that entry i (uniform) of a packed batch belongs to: a prefix sum per lane, all of them in one load.
+__device__ __forceinline__ int seq_at(kern_ints_t off, int n_seq, int i) {
+  const int lane = threadIdx.x & 63;
+  return __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < n_seq - 1 && i >= off[min(lane, n_seq - 1) + 1]));
 }
 
 // The rows of kTok tokens: queries (n_q heads, into q_out), keys and values (n_kv heads each, into the pages).
 template <int kTok>
-__device__ __forceinline__ void append_rows(const AppendArgs &a, TurnTable<kTok> &turns, int (&slots)[kTok], int token0, int n_q, int n_kv) {
+__device__ __forceinline__ void append_rows(AppendKernArgs &a, TurnTable<kTok> &turns, int (&slots)[kTok], int token0, int n_q, int n_kv) {
   const int n_tok = min(kTok, a.total - token0), tid = threadIdx.x, j = tid & (kRowLanes - 1);
   const int rows_per = n_q + 2 * n_kv, n_rows = n_tok * rows_per;
   struct Row {
@@ -98,16 +101,36 @@ __device__ __forceinline__ void append_rows(const AppendArgs &a, TurnTable<kTok>
     w.part = row_part(a, j, w.kind != 2);
     return w;
   };
-  if (n_kv > 0 && tid < n_tok) {
-    const int t = token0 + tid, b = seq_at(a.off, a.n_seq, t), at = a.start[b] + (t - a.off[b]);
-    const int page = a.block_table[(size_t)b * a.max_pages + (at >> a.page_shift)];
-    slots[tid] = page >= 0 && page < a.n_pages ? (page << a.page_shift) + (at & ((1 << a.page_shift) - 1)) : -1;
+  // a thread's first row is on its way while angles and slots are looked up
+  int r = tid / kRowLanes;
+  Row w{};
+  u32x4 first{}, second{};
+  if (r < n_rows) {
+    w = row_at(r);
+    first = w.src[w.part.first];
+    second = w.src[w.part.second];
+  }
+  if (n_kv > 0 && tid < 64) {  // the first wave, a lane per token
+    int b = 0, at = 0;
+#pragma unroll
+    for (int i = 0; i < kTok; ++i) {
+      const int token = min(token0 + i, a.total - 1), owner = seq_at(a.off, a.n_seq, token), place = a.start[owner] + token - a.off[owner];
+      b = tid == i ? owner : b;
+      at = tid == i ? place : at;
+    }
+    if (tid < n_tok) {
+      const int page = a.block_table[(size_t)b * a.max_pages + (at >> a.page_shift)];
+      slots[tid] = page >= 0 && page < a.n_pages ? (page << a.page_shift) + (at & ((1 << a.page_shift) - 1)) : -1;
+    }
   }
   if (a.pairs > 0) fill_turns(a, turns, token0, n_tok);
   __syncthreads();
-  for (int r = tid / kRowLanes; r < n_rows; r += blockDim.x / kRowLanes) {
-    const Row w = row_at(r);
-    u32x4 first = w.src[w.part.first], second = w.src[w.part.second];
+  for (bool more = false; r < n_rows; r += blockDim.x / kRowLanes, more = true) {
+    if (more) {
+      w = row_at(r);
+      first = w.src[w.part.first];
+      second = w.src[w.part.second];
+    }
     if (w.part.turned) {
       float x[16];
       turn16(a, first, second, &turns.cs[w.tok][8 * j], &turns.sn[w.tok][8 * j], x);
@@ -127,70 +150,73 @@ __device__ __forceinline__ void append_rows(const AppendArgs &a, TurnTable<kTok>
   }
 }
 
-template <int kTok>
-__global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a) {
-  __shared__ __attribute__((aligned(16))) TurnTable<kTok> turns;
-  __shared__ int slots[kTok];
-  append_rows<kTok>(a, turns, slots, blockIdx.x * kTok, a.q ? a.Hq : 0, a.Hkv);
+// A block takes one token, a thread 16 columns of one of its rows: nothing but the one memory trip behind the look-ups.  8191 tokens 38.8 us (5.2 TB/s, the
+// rate of a large copy), of two tokens a block 41.8, four 43.1, eight 46.3; 64 tokens 4.5, 5.7, 8.2, 12.7.
+__global__ __launch_bounds__(kAppendMaxThreads) void k_append(AppendArgs) {
+  AppendKernArgs &a = FKV_KERN_ARGS(AppendKernArgs);
+  __shared__ __attribute__((aligned(16))) TurnTable<1> turns;
+  __shared__ int slots[1];
+  append_rows<1>(a, turns, slots, blockIdx.x, a.q ? a.Hq : 0, a.Hkv);
 }
 
-// One scale block of one head, a wave's work: of its rows 0 .. kBlock - 1 (of kHeadDim bytes at `codes`) first .. last - 1 may be new, and
-// earlier tokens lie in those ahead of them.  A thread has row p * kRowLanes + lane / kRowLanes of step p.  live(p): that row is
-// new indeed; load(p, chunks) fetches its two 16-byte chunks, value(p, chunks, x) gives their 16 numbers.  No new row: nothing is written.
-template <int kBlock, typename Live, typename Load, typename Value>
-__device__ __forceinline__ void store_block(int first, int last, uint8_t *codes, float *scale, Live live, Load load, Value value, RowPart part) {
+// One scale block of one head, a wave's work: of its rows 0 .. kBlock - 1 (of kHeadDim bytes at `codes`) those of is_new are new, and
+// earlier tokens lie in the `kept` rows at its begin.  A thread has row p * kRowLanes + lane / kRowLanes of step p, of which value(p, x) gives the
+// 16 numbers of its two chunks.  No new row: nothing is written.
+template <int kBlock, typename Value>
+__device__ __forceinline__ void store_block(int kept, const bool (&is_new)[kBlock / kRowLanes], uint8_t *codes, float *scale, Value value, RowPart part) {
   constexpr int kSteps = kBlock / kRowLanes;
-  const int lane = threadIdx.x & 63, j = lane & (kRowLanes - 1), sub = lane / kRowLanes;
-  u32x4 raw[kSteps][2];
-  bool is_new[kSteps], any = false;
-#pragma unroll
-  for (int p = 0; p < kSteps; ++p) {
-    const int i = p * kRowLanes + sub;
-    is_new[p] = i >= first && i < last && live(p);
-    any |= is_new[p];
-    if (is_new[p]) load(p, raw[p]);
-  }
+  const int lane = threadIdx.x & 63, sub = lane / kRowLanes;
+  const float old = kept > 0 ? *scale : 0.f;
   float amax = 0.f;
+  bool any = false;
 #pragma unroll
   for (int p = 0; p < kSteps; ++p) {
+    any |= is_new[p];
     if (is_new[p]) {
       float x[16];
-      value(p, raw[p], x);
+      value(p, x);
 #pragma unroll
       for (int e = 0; e < 16; ++e) amax = fmaxf(amax, is_finite(x[e]) ? __builtin_fabsf(x[e]) : 0.f);
     }
   }
   if (__builtin_amdgcn_ballot_w64(any) == 0ull) return;
   amax = wave_fmax(amax);
-  const float old = first > 0 ? *scale : 0.f, now = fmaxf(scale_for(amax), old), inv = 1.f / now;
-  if (first > 0 && now > old) {
+  const float now = fmaxf(scale_for(amax), old), inv = 1.f / now;
+  if (kept > 0 && now > old) {
     const float ratio = old / now;
-    for (int i = sub; i < first; i += kRowLanes) {
-      u32x4 *row = reinterpret_cast<u32x4 *>(codes + i * kHeadDim) + j;
-      u32x4 c = *row;
+    for (int i = lane; i < kept * 8; i += 64) {  // 16 codes each
+      u32x4 *at = reinterpret_cast<u32x4 *>(codes) + i;
+      u32x4 c = *at;
 #pragma unroll
       for (int e = 0; e < 4; ++e) c[e] = rescale4(c[e], ratio);
-      *row = c;
+      *at = c;
     }
   }
 #pragma unroll
   for (int p = 0; p < kSteps; ++p) {
     if (is_new[p]) {
       float x[16];
-      value(p, raw[p], x);
+      value(p, x);
       u32x2 *row = reinterpret_cast<u32x2 *>(codes + (p * kRowLanes + sub) * kHeadDim);
-      row[part.first] = encode8(x, inv);
-      row[part.second] = encode8(x + 8, inv);
+      const u32x2 first = encode8(x, inv), second = encode8(x + 8, inv);
+      if (part.second == part.first + 1) {
+        *reinterpret_cast<u32x4 *>(row + part.first) = u32x4{first[0], first[1], second[0], second[1]};
+      } else {
+        row[part.first] = first;
+        row[part.second] = second;
+      }
     }
   }
   if (lane == 0) *scale = now;
 }
 
-// Blocks of the grid: a scale block of a sequence for K, one for V (a wave for each head), and so on, then kAppendTok tokens' queries each.
-constexpr int kAppendTok = 8;
+// Blocks of the grid: a scale block of a sequence for K, one for V (a wave for each head), and so on, then kAppendTok tokens' queries each (11000
+// tokens: 8 of them 61.5 us, 4 59.2, 2 57.2, 1 64.9, which leaves half of the threads idle).
+constexpr int kAppendTok = 2;
 
 template <int kBlock>
-__global__ __launch_bounds__(kMaxKvHeads * 64) void k_append_quant(AppendArgs a) {
+__global__ __launch_bounds__(kMaxKvHeads * 64) void k_append_quant(AppendArgs) {
+  AppendKernArgs &a = FKV_KERN_ARGS(AppendKernArgs);
   constexpr int kTok = kBlock > kAppendTok ? kBlock : kAppendTok;
   __shared__ __attribute__((aligned(16))) TurnTable<kTok> turns;
   const int block = blockIdx.x, n_blk = 2 * a.blk[a.n_seq];
@@ -204,71 +230,86 @@ __global__ __launch_bounds__(kMaxKvHeads * 64) void k_append_quant(AppendArgs a)
   const int start = a.start[b], end = start + (a.off[b + 1] - a.off[b]);
   const int tok0 = (start / kBlock + (at - a.blk[b])) * kBlock;  // the block's first token
   const int first = max(start - tok0, 0), last = min(end - tok0, kBlock);
-  const int page = a.block_table[(size_t)b * a.max_pages + (tok0 >> a.page_shift)];
   const int token0 = a.off[b] + (tok0 + first - start);  // packed index of the first new token
+  const int page = a.block_table[(size_t)b * a.max_pages + (tok0 >> a.page_shift)];
   const bool turn = !is_v && a.pairs > 0;
+  const int h = threadIdx.x >> 6, lane = threadIdx.x & 63, j = lane & (kRowLanes - 1);
+  const RowPart part = row_part(a, j, turn);
+  // The rows are on their way while page and angles are looked up.
+  const uint16_t *src = (is_v ? a.v : a.k) + h * kHeadDim;
+  const int64_t stride = is_v ? a.v_stride : a.k_stride;
+  const int sub = lane / kRowLanes - first;  // of a thread's row among the new ones, in step 0
+  u32x4 raw[kBlock / kRowLanes][2];
+  bool is_new[kBlock / kRowLanes];
+#pragma unroll
+  for (int p = 0; p < kBlock / kRowLanes; ++p) {
+    const int i = p * kRowLanes + sub;
+    is_new[p] = i >= 0 && i < last - first;
+    const u32x4 *r = reinterpret_cast<const u32x4 *>(src + (int64_t)(token0 + min(max(i, 0), last - first - 1)) * stride);
+    raw[p][0] = r[part.first];
+    raw[p][1] = r[part.second];
+  }
   if (turn) {
     fill_turns(a, turns, token0, last - first);
     __syncthreads();
   }
   if (page < 0 || page >= a.n_pages) return;
-  const int h = threadIdx.x >> 6, lane = threadIdx.x & 63, j = lane & (kRowLanes - 1), in_page = tok0 & ((1 << a.page_shift) - 1);
-  const size_t row = (((size_t)page * a.Hkv + h) << a.page_shift) + in_page;
-  const RowPart part = row_part(a, j, turn);
-  const uint16_t *src = (is_v ? a.v : a.k) + h * kHeadDim;
-  const int64_t stride = is_v ? a.v_stride : a.k_stride;
-  const int sub = lane / kRowLanes - first;  // of a thread's row among the new ones, in step 0
+  const size_t row = (((size_t)page * a.Hkv + h) << a.page_shift) + (tok0 & ((1 << a.page_shift) - 1));
   store_block<kBlock>(
-      first, last, (is_v ? a.v_codes : a.k_codes) + row * kHeadDim, (is_v ? a.v_scale : a.k_scale) + row / kBlock,
-      [](int) { return true; },
-      [&](int p, u32x4 (&raw)[2]) {
-        const u32x4 *r = reinterpret_cast<const u32x4 *>(src + (int64_t)(token0 + p * kRowLanes + sub) * stride);
-        raw[0] = r[part.first];
-        raw[1] = r[part.second];
-      },
-      [&](int p, const u32x4 (&raw)[2], float (&x)[16]) {
+      first, is_new, (is_v ? a.v_codes : a.k_codes) + row * kHeadDim, (is_v ? a.v_scale : a.k_scale) + row / kBlock,
+      [&](int p, float (&x)[16]) {
         if (part.turned) {
           const int i = p * kRowLanes + sub;
-          turn16(a, raw[0], raw[1], &turns.cs[i][8 * j], &turns.sn[i][8 * j], x);
+          turn16(a, raw[p][0], raw[p][1], &turns.cs[i][8 * j], &turns.sn[i][8 * j], x);
         } else {
-          unpack8(raw[0], x);
-          unpack8(raw[1], x + 8);
+          unpack8(raw[p][0], x);
+          unpack8(raw[p][1], x + 8);
         }
       },
       part);
 }
 
-// KVCompress into the cache in 8 bits: block (scale block of kept rows, K or V), a wave for each head.
+// KVCompress into the cache in 8 bits: a wave for a scale block of kept rows, of K or V and one head (heads fastest, then K and V).
+constexpr int kGatherWaves = 4;
+
 template <int kBlock>
-__global__ __launch_bounds__(kMaxKvHeads * 64) void k_gather_quant(QuantGatherArgs a) {
-  const int at = blockIdx.x, b = seq_at(a.blk, a.n_seq, at), is_v = blockIdx.y;
+__global__ __launch_bounds__(kGatherWaves * 64) void k_gather_quant(QuantGatherArgs) {
+  GatherKernArgs &a = FKV_KERN_ARGS(GatherKernArgs);
+  constexpr int kSteps = kBlock / kRowLanes;
+  const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * kGatherWaves + (threadIdx.x >> 6)), n_src = a.src[1] ? 2 : 1;
+  const int line = (int)((uint32_t)unit / (uint32_t)a.Hkv), h = unit - line * a.Hkv;
+  const int at = n_src == 2 ? line >> 1 : line, is_v = n_src == 2 ? line & 1 : 0;
+  if (at >= a.blk[a.n_seq]) return;
+  const int b = seq_at(a.blk, a.n_seq, at), lane = threadIdx.x & 63, j = lane & (kRowLanes - 1);
   const int tok0 = (at - a.blk[b]) * kBlock, last = min(a.cnt_off[b + 1] - a.cnt_off[b] - tok0, kBlock);
   const int page = a.block_table[(size_t)b * a.max_pages + (tok0 >> a.page_shift)];
-  if (page < 0 || page >= a.n_pages) return;
-  const int h = threadIdx.x >> 6, lane = threadIdx.x & 63, j = lane & (kRowLanes - 1), in_page = tok0 & ((1 << a.page_shift) - 1);
-  const size_t row = (((size_t)page * a.Hkv + h) << a.page_shift) + in_page;
-  const int base = a.cu[b], n = a.cu[b + 1] - base;
   const int all = a.idx[(size_t)h * a.total_rows + a.cnt_off[b] + tok0 + min(lane & (kBlock - 1), last - 1)];  // a lane each
-  int kept[kBlock / kRowLanes];
-#pragma unroll
-  for (int p = 0; p < kBlock / kRowLanes; ++p) kept[p] = __shfl(all, p * kRowLanes + lane / kRowLanes);
+  const int base = a.cu[b], n = a.cu[b + 1] - base;
   const uint16_t *src = a.src[is_v] + h * kHeadDim;
+  u32x4 raw[kSteps][2];
+  bool is_new[kSteps];
+#pragma unroll
+  for (int p = 0; p < kSteps; ++p) {
+    const int i = p * kRowLanes + lane / kRowLanes, kept = __shfl(all, i);
+    is_new[p] = i < last && kept >= 0;
+    const u32x4 *r = reinterpret_cast<const u32x4 *>(src + (int64_t)(base + min(max(kept, 0), n - 1)) * a.Hkv * kHeadDim) + 2 * j;
+    raw[p][0] = r[0];
+    raw[p][1] = r[1];
+  }
+  if (page < 0 || page >= a.n_pages) return;
+  const size_t row = (((size_t)page * a.Hkv + h) << a.page_shift) + (tok0 & ((1 << a.page_shift) - 1));
   store_block<kBlock>(
-      0, last, a.codes[is_v] + row * kHeadDim, a.scale[is_v] + row / kBlock, [&](int p) { return kept[p] >= 0; },
-      [&](int p, u32x4 (&raw)[2]) {
-        const u32x4 *r = reinterpret_cast<const u32x4 *>(src + (int64_t)(base + min(kept[p], n - 1)) * a.Hkv * kHeadDim);
-        raw[0] = r[2 * j];
-        raw[1] = r[2 * j + 1];
-      },
-      [&](int, const u32x4 (&raw)[2], float (&x)[16]) {
-        unpack8(raw[0], x);
-        unpack8(raw[1], x + 8);
+      0, is_new, a.codes[is_v] + row * kHeadDim, a.scale[is_v] + row / kBlock,
+      [&](int p, float (&x)[16]) {
+        unpack8(raw[p][0], x);
+        unpack8(raw[p][1], x + 8);
       },
       RowPart{2 * j, 2 * j + 1, false});
 }
 
 hipError_t launch_append(const AppendArgs &a, hipStream_t s) {
-  hipLaunchKernelGGL((k_append<1>), dim3(a.total), dim3(kAppendThreads), 0, s, a);
+  const int threads = (((a.q ? a.Hq : 0) + 2 * a.Hkv) * kRowLanes + 63) / 64 * 64;
+  hipLaunchKernelGGL(k_append, dim3(a.total), dim3(threads), 0, s, a);
   return hipGetLastError();
 }
 
@@ -281,7 +322,8 @@ hipError_t launch_append_quant(const AppendArgs &a, int block, hipStream_t s) {
 }
 
 hipError_t launch_gather_quant(const QuantGatherArgs &a, int block, hipStream_t s) {
-  const dim3 grid(a.blk[a.n_seq], a.src[1] ? 2 : 1), threads(a.Hkv * 64);
+  const int units = a.blk[a.n_seq] * a.Hkv * (a.src[1] ? 2 : 1);
+  const dim3 grid((units + kGatherWaves - 1) / kGatherWaves), threads(kGatherWaves * 64);
   if (block == 16) hipLaunchKernelGGL((k_gather_quant<16>), grid, threads, 0, s, a);
   else if (block == 32) hipLaunchKernelGGL((k_gather_quant<32>), grid, threads, 0, s, a);
   else hipLaunchKernelGGL((k_gather_quant<64>), grid, threads, 0, s, a);
