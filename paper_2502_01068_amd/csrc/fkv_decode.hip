@@ -340,7 +340,7 @@ DecodePlan plan_decode(DecodeArgs &a, int n_cu, int waves, bool whole_rounds) {
   //   against 56 us, of 1280-2560 45.6 against 48; but 320 rows 54 against 47.7); rows of up to 12 tiles, where a fold
   //   costs more than it saves (160 rows of 250 tokens 7.4 against 13.9).
   //   Pieces: few rows, or few tiles per CU (128 rows of 1000 tokens 14.2 against 17 us; of 5000, 63 against 55.7).
-  const int whole_tiles = whole_rounds ? 16 : 12;  // in 8 bits (a row of 512 tokens 7.8 us in two pieces, 7.2 whole; of 768 7.9, 8.5)
+  const int whole_tiles = whole_rounds ? kDecQuantWhole : 12;  // in 8 bits (a row of 512 tokens 7.8 us in two pieces, 7.2 whole; of 768 7.9, 8.5)
   const int rows = a.n_seq * a.Hkv;
   const int per_cu = (rows + n_cu - 1) / n_cu;
   const bool even = 10 * rows >= 9 * per_cu * n_cu && 2 * longest * a.n_seq <= 3 * tiles;

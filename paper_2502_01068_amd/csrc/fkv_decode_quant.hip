@@ -16,6 +16,7 @@
 // compiler would wait for all).  Page entries come 32 tiles at a time, a lane each.
 //
 // Work is spread and rows folded as in fkv_decode.hip.
+#include <algorithm>
 #include <type_traits>
 
 #include "fkv_decode_common.h"
@@ -342,11 +343,21 @@ __global__ __launch_bounds__(kWaves * 64, 2) void k_decode_quant(DecodeQuantArgs
 }
 
 hipError_t launch_decode_quant(DecodeQuantArgs &a, int n_cu, hipStream_t s) {
-  // Blocks of 8 waves, one to a CU (149 KB of LDS), or where there are more rows than CUs two of 4 waves each, so that one block's start is
-  // covered by the other.  us, 8 waves and 4: 256 rows of 2048-2560 tokens 29.3, 30.6; one sequence of 131072 (8 rows) 47.1, 49.0; 128 rows of
-  // 1000 12.5, 12.3; but 512 rows of 2000 50.3, 45.4; of 200 13.5, 9.9; 384 rows of 500-1000 25.2, 23.0; 264 of 600-1200 21.1, 17.5.
-  const bool wide = a.d.n_seq * a.d.Hkv <= n_cu;
-  const DecodePlan plan = wide ? plan_decode(a.d, n_cu, 8, true) : plan_decode(a.d, 2 * n_cu, 4, true);
+  // Blocks of 8 waves, one to a CU (149 KB of LDS); of 4
+  //   where there are more rows than CUs, two to a CU, so that one block's start is covered by the other.  us, 8 waves and 4: 256 rows of 2048-2560
+  //   tokens 29.3, 30.6; one sequence of 131072 (8 rows) 47.1, 49.0; 128 rows of 1000 12.5, 12.3; but 512 rows of 2000 50.3, 45.4; of 200 13.5, 9.9;
+  //   384 rows of 500-1000 25.2, 23.0; 264 of 600-1200 21.1, 17.5;
+  //   where a tile for each wave leaves half of the CUs idle: the SIMDs then have one wave each.  One sequence of 1024 tokens 7.9, 7.3, 2048 7.9,
+  //   7.3; 3000 8.0, 8.3.  Not where rows stay whole: 512 7.2, 7.5.
+  const int rows = a.d.n_seq * a.d.Hkv;
+  int64_t tiles = 0, longest = 0;
+  for (int b = 0; b < a.d.n_seq; ++b) {
+    const int64_t t = (a.d.off[b + 1] - a.d.off[b] + kDecTile - 1) / kDecTile;
+    tiles += t * a.d.Hkv;
+    longest = std::max(longest, t);
+  }
+  const bool few = tiles <= 2 * n_cu && longest > kDecQuantWhole, wide = rows <= n_cu && !few;
+  const DecodePlan plan = wide ? plan_decode(a.d, n_cu, 8, true) : plan_decode(a.d, few ? n_cu : 2 * n_cu, 4, true);
   auto launch = [&](auto aligned_t, auto waves_t) {
     constexpr int kWaves = decltype(waves_t)::value;
     hipLaunchKernelGGL((k_decode_quant<decltype(aligned_t)::value, kWaves>), dim3(plan.blocks), dim3(kWaves * 64), 0, s, a);

@@ -224,6 +224,7 @@ struct DecodeArgs {
   int max_pages, page_shift, n_pages;
 };
 constexpr int kDecWaves = 4;  // of a block, over a bf16 cache
+constexpr int kDecQuantWhole = 16;  // tiles up to which a row stays whole over a cache in 8 bits
 struct DecodePlan {
   int blocks;
   bool aligned;  // every row is whole or cut into equal pieces (piece0), one per block; else the line of all tiles is cut into equal shares
