@@ -256,7 +256,7 @@ int fkv_decode_attention_paged(fkv_ctx *ctx, const fkv_shape *shape, const void 
 
 /* Rotary position embedding (host struct, read during the call only): columns x, y of pair i of a head's row become
  * x cos(phi) - y sin(phi) and y cos(phi) + x sin(phi), phi = position * inv_freq[i].  The angle is reduced exactly (positions are
- * whole numbers), sine and cosine are fp32 values within 2 ulp, and a result is rounded once to what it is stored as. */
+ * whole numbers), sine and cosine are fp32 values within 2^-22, and a result is rounded once to what it is stored as. */
 typedef struct fkv_rope {
   int32_t rotary_dim;     /* r: the first r columns of a row take part, the others pass unchanged; a multiple of 16, 16 <= r <= d */
   int32_t interleaved;    /* 0: columns i and i + r/2 are pair i; 1: columns 2i and 2i + 1 */
@@ -273,14 +273,16 @@ typedef struct fkv_new_tokens {
   const int32_t *positions; /* device [sum n_new] int32, the tokens' positions (any sign; not their places in the cache, which fall behind
                              * them once KVCompress has dropped tokens); required with a rope, unused without */
   const int32_t *n_cached;  /* host [B] >= 0: tokens of the sequence that the cache holds before the call */
-  const int32_t *n_new;     /* host [B] >= 0 */
+  const int32_t *n_new;     /* host [B] >= 0, at most 2^22 in all; without any, the pointers above may be NULL */
 } fkv_new_tokens;
 
 /* The new tokens of each sequence into its pages behind the n_cached_b tokens there (serving counterpart of C <- update(K, V),
  * Algorithm 1): logical tokens n_cached_b .. n_cached_b + n_new_b - 1 receive v and, turned by `rope` (NULL: as they are), k; q_out
  * receives the queries turned the same way.  Pools and table as above; the sequences of a call must not write the same slot.  Other slots
  * are not written; a table entry outside the pool writes nothing.  Needs no workspace: the context only names the device, and calls
- * of one context on different streams may overlap.  Only n_seq and the head counts of `shape` are used. */
+ * of one context on different streams may overlap on the GPU.  Only n_seq and the head counts of `shape` are used.  Counts are read during
+ * the call: a graph that holds it appends at the same places at every replay (positions, rows and table are read from the device).
+ * (fkv_profile_read counts the launch as "k_gather".) */
 int fkv_append_kv_paged(fkv_ctx *ctx, const fkv_shape *shape, const fkv_rope *rope, const fkv_new_tokens *tokens,
                         const int32_t *block_table, int32_t max_pages_per_seq, int32_t page_size, int64_t n_pages,
                         void *k_pages, void *v_pages, void *stream);

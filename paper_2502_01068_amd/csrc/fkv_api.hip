@@ -1209,7 +1209,7 @@ uint64_t turns_of(double f) {
   return (bits >> 63) != 0 ? 0 - turns : turns;
 }
 
-constexpr int64_t kAppendMaxTokens = 1 << 28;  // block numbers of a launch stay below 2^31
+constexpr int64_t kAppendMaxTokens = 1 << 22;  // a launch has less than 2^32 threads, at most 640 a token
 
 int fill_append(const Resolved &r, const fkv_rope *rope, const fkv_new_tokens *t, const Paging &pg, AppendArgs *a) {
   if (!t || !t->n_cached || !t->n_new) return FKV_ENULL;
@@ -1219,7 +1219,7 @@ int fill_append(const Resolved &r, const fkv_rope *rope, const fkv_new_tokens *t
     if (t->n_cached[b] < 0 || t->n_new[b] < 0) return FKV_EINVAL;
     if ((int64_t)t->n_cached[b] + t->n_new[b] > (int64_t)pg.max_pages * pg.page_size) return FKV_EINVAL;
     total += t->n_new[b];
-    if (total > kAppendMaxTokens) return FKV_EINVAL;
+    if (total > kAppendMaxTokens) return FKV_EUNSUPPORTED;
     a->start[b] = t->n_cached[b];
     a->off[b + 1] = (int)total;
   }
@@ -1282,10 +1282,13 @@ void fill_gather_quant(QuantGatherArgs &g, const Resolved &r, const void *k, con
   for (int b = 0; b <= r.n_seq; ++b) g.cu[b] = r.cu[b];
 }
 
-int check_budget_pages(const Resolved &r, const int32_t *budget_per_seq, const Paging &pg) {
+// Counts of a gather into pages: as those of the bf16 pages (check_paged_gather), whose bound on the rows also keeps the launch's threads below 2^32.
+int check_quant_gather(const Resolved &r, const int32_t *budget_per_seq, const Paging &pg, QuantGatherArgs *g) {
+  const int rc = check_counts(r, budget_per_seq, g->cnt_off);
+  if (rc != FKV_OK) return rc;
   for (int b = 0; b < r.n_seq; ++b)
     if (budget_per_seq[b] > (int64_t)pg.max_pages * pg.page_size) return FKV_EINVAL;
-  return FKV_OK;
+  return (int64_t)g->cnt_off[r.n_seq] * r.Hkv > (INT32_MAX >> 5) ? FKV_EINVAL : FKV_OK;
 }
 }  // namespace
 
@@ -1354,8 +1357,7 @@ int fkv_gather_kv_paged_quant(fkv_ctx *ctx, const fkv_shape *shape, const void *
   if (rc != FKV_OK) return rc;
   if ((v == nullptr) != (pages->v_pages == nullptr)) return FKV_ENULL;
   QuantGatherArgs g{};
-  rc = check_counts(r, budget_per_seq, g.cnt_off);
-  if (rc == FKV_OK) rc = check_budget_pages(r, budget_per_seq, pg);
+  rc = check_quant_gather(r, budget_per_seq, pg, &g);
   if (rc != FKV_OK) return rc;
   if (misaligned(k) || misaligned(v) || misaligned(idx_kv)) return FKV_EALIGN;
   rc = check_ctx(ctx, r);
@@ -1377,8 +1379,7 @@ int fkv_compress_kv_paged_quant(fkv_ctx *ctx, const fkv_shape *shape, const void
   rc = check_quant_pages(pages, r.Hkv, false, &pg);
   if (rc != FKV_OK) return rc;
   QuantGatherArgs g{};
-  rc = check_counts(r, budget_per_seq, g.cnt_off);
-  if (rc == FKV_OK) rc = check_budget_pages(r, budget_per_seq, pg);
+  rc = check_quant_gather(r, budget_per_seq, pg, &g);
   if (rc != FKV_OK) return rc;
   if (misaligned(q_win) || misaligned(k) || misaligned(v) || misaligned(idx_kv)) return FKV_EALIGN;
   rc = check_ctx(ctx, r);

@@ -159,6 +159,23 @@ def test_gather(ctx, lengths, budget, hkv, page, block):
             assert (np.where(sel[:, None], fresh[0].cpu().numpy()[p, :, t % page], put[p, :, t % page]) & 127 == put[p, :, t % page] & 127).all()
 
 
+def test_gather_indices_repeat_and_run_over(ctx):
+    """An index twice is a row twice; one beyond its sequence is clamped into it, as by the other gathers."""
+    rng = np.random.default_rng(31)
+    shape = fk.make_shape([40, 30], n_q_heads=2, n_kv_heads=2)
+    k = bits(rng, 70, 2, 128)
+    idx = np.stack([[3, 3, 3, 39, 40, 1000, 0, 7, 2 ** 31 - 1, 29, 30, 0, 0, 5, 6, 6]] * 2).astype(np.int32)
+    table = np.array([[0], [1]], np.int32)
+    codes, scales = noise_pools(rng, 2, 2, 16, 16)
+    got = up((codes, scales))
+    ctx.fkv_gather_kv_paged_quant(shape, dev(k), dev(k), torch.from_numpy(idx).cuda(), 8, torch.from_numpy(table).cuda(), *got)
+    for c, s in zip(codes, scales):
+        for b, (row, n) in enumerate(((0, 40), (40, 30))):
+            own = np.minimum(idx[:, 8 * b:8 * b + 8].T, n - 1)
+            paged.append_quant(c, s, paged.bf16_to_f64(k[row:row + n])[own, np.arange(2)], 0, table[b])
+    same(got, codes, scales)
+
+
 def test_pages_outside_the_pool(ctx):
     rng = np.random.default_rng(30)
     shape = fk.make_shape(64, n_q_heads=2, n_kv_heads=2)

@@ -73,6 +73,8 @@ def test_append_refuses(lib, quant):
     for cached, new in (((-1, 0), (1, 1)), ((0, 0), (1, -1)), ((250, 0), (7, 1)), ((0, 0), (1 << 30, 1))):
         assert call(tokens(cached, new)) == fk.FKV_EINVAL
     assert call(tokens((249, 0), (7, 1))) == fk.FKV_ENULL  # the last slot of the table: fits
+    big = dict(max_pages_per_seq=1 << 20)
+    assert call(tokens((0, 5), ((1 << 22) - 1, 1)), **big) == fk.FKV_ENULL and call(tokens((0, 5), (1 << 22, 1)), **big) == fk.FKV_EUNSUPPORTED
     assert call(tokens(k_stride=1016)) == fk.FKV_EINVAL and call(tokens(k_stride=1028)) == fk.FKV_EALIGN and call(tokens(k_stride=-1024)) == fk.FKV_EINVAL
     assert call(tokens(q_stride=4088)) == fk.FKV_EINVAL and call(tokens(v_stride=1 << 40)) == fk.FKV_EINVAL
     assert call(tokens(q_out_stride=8192)) == fk.FKV_EINVAL      # in place at another stride
