@@ -278,7 +278,7 @@ typedef struct fkv_new_tokens {
 
 /* The new tokens of each sequence into its pages behind the n_cached_b tokens there (serving counterpart of C <- update(K, V),
  * Algorithm 1): logical tokens n_cached_b .. n_cached_b + n_new_b - 1 receive v and, turned by `rope` (NULL: as they are), k; q_out
- * receives the queries turned the same way.  Pools and table as above; the sequences of a call must not write the same slot.  Other slots
+ * receives the queries turned the same way.  n_cached_b + n_new_b <= 2^30.  Pools and table as above; the sequences of a call must not write the same slot.  Other slots
  * are not written; a table entry outside the pool writes nothing.  Needs no workspace: the context only names the device, and calls
  * of one context on different streams may overlap on the GPU.  Only n_seq and the head counts of `shape` are used.  Counts are read during
  * the call: a graph that holds it appends at the same places at every replay (positions, rows and table are read from the device).
@@ -310,7 +310,7 @@ typedef struct fkv_quant_pages {
 /* fkv_append_kv_paged, fkv_gather_kv_paged, fkv_compress_kv_paged and fkv_decode_attention_paged on such a cache.  Appending: the
  * sequences of a call must not write into the same block.  Gathering: rows of negative indices are not written and do not count
  * towards a scale.  A table entry outside the pool writes nothing, and is clamped into it by the decode call.
- * Decoding: n_per_seq[b] >= 0, and a sequence without tokens gives zeros (the padding of a batch); any fp32 scales are read, not only powers
+ * Decoding: 0 <= n_per_seq[b] <= 2^30, and a sequence without tokens gives zeros (the padding of a batch); any fp32 scales are read, not only powers
  * of two.  Both contractions are accumulated in fp32 from exact products of what the codes stand for. */
 int fkv_append_kv_paged_quant(fkv_ctx *ctx, const fkv_shape *shape, const fkv_rope *rope, const fkv_new_tokens *tokens,
                               const fkv_quant_pages *pages, void *stream);

@@ -1209,6 +1209,7 @@ uint64_t turns_of(double f) {
   return (bits >> 63) != 0 ? 0 - turns : turns;
 }
 
+constexpr int64_t kPagedMaxTokens = 1 << 30;  // of a sequence: a tile's or block's last place stays below 2^31
 constexpr int64_t kAppendMaxTokens = 1 << 22;  // a launch has less than 2^32 threads, at most 640 a token
 
 int fill_append(const Resolved &r, const fkv_rope *rope, const fkv_new_tokens *t, const Paging &pg, AppendArgs *a) {
@@ -1217,7 +1218,9 @@ int fill_append(const Resolved &r, const fkv_rope *rope, const fkv_new_tokens *t
   a->off[0] = 0;
   for (int b = 0; b < r.n_seq; ++b) {
     if (t->n_cached[b] < 0 || t->n_new[b] < 0) return FKV_EINVAL;
-    if ((int64_t)t->n_cached[b] + t->n_new[b] > (int64_t)pg.max_pages * pg.page_size) return FKV_EINVAL;
+    const int64_t n = (int64_t)t->n_cached[b] + t->n_new[b];
+    if (n > (int64_t)pg.max_pages * pg.page_size) return FKV_EINVAL;
+    if (n > kPagedMaxTokens) return FKV_EUNSUPPORTED;
     total += t->n_new[b];
     if (total > kAppendMaxTokens) return FKV_EUNSUPPORTED;
     a->start[b] = t->n_cached[b];
@@ -1412,6 +1415,7 @@ int fkv_decode_attention_paged_quant(fkv_ctx *ctx, const fkv_shape *shape, const
   int64_t tot = 0;
   for (int b = 0; b < r.n_seq; ++b) {
     if (n_per_seq[b] < 0 || n_per_seq[b] > (int64_t)pg.max_pages * pg.page_size) return FKV_EINVAL;
+    if (n_per_seq[b] > kPagedMaxTokens) return FKV_EUNSUPPORTED;
     tot += n_per_seq[b];
     if (tot > INT32_MAX) return FKV_EINVAL;
     a.d.off[b + 1] = (int)tot;

@@ -201,8 +201,8 @@ __device__ __forceinline__ void append_rows(AppendKernArgs &a, TurnTable<kTok> &
   }
 }
 
-// A block takes one token, a thread 16 columns of one of its rows: nothing but the one memory trip behind the look-ups.  8191 tokens 38.8 us (5.2 TB/s, the
-// rate of a large copy), of two tokens a block 41.8, four 43.1, eight 46.3; 64 tokens 4.5, 5.7, 8.2, 12.7.
+// A block takes one token, a thread 16 columns of one of its rows: nothing but the one memory trip behind the look-ups.  8191 tokens 37.2 us (5.4 TB/s; a large
+// copy 5.2), 64 tokens 4.3; in a form that took longer to look up, 38.8 and 4.5, two tokens a block 41.8 and 5.7, four 43.1 and 8.2, eight 46.3 and 12.7.
 __global__ __launch_bounds__(kAppendMaxThreads) void k_append(AppendArgs) {
   AppendKernArgs &a = FKV_KERN_ARGS(AppendKernArgs);
   __shared__ __attribute__((aligned(16))) TurnTable<1> turns;
@@ -265,7 +265,7 @@ __device__ __forceinline__ void store_block(int kept, const bool (&is_new)[kBloc
 }
 
 // Blocks of the grid: a scale block of a sequence for K, one for V (a wave for each head), and so on, then kAppendTok tokens' queries each (11000
-// tokens: 8 of them 61.5 us, 4 59.2, 2 57.2, 1 64.9, which leaves half of the threads idle).
+// tokens, at 54.3 us now: 8 of them 61.5, 4 59.2, 2 57.2, 1 64.9, which leaves half of the threads idle).
 constexpr int kAppendTok = 2;
 
 template <int kBlock>

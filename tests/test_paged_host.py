@@ -73,7 +73,8 @@ def test_append_refuses(lib, quant):
     for cached, new in (((-1, 0), (1, 1)), ((0, 0), (1, -1)), ((250, 0), (7, 1)), ((0, 0), (1 << 30, 1))):
         assert call(tokens(cached, new)) == fk.FKV_EINVAL
     assert call(tokens((249, 0), (7, 1))) == fk.FKV_ENULL  # the last slot of the table: fits
-    big = dict(max_pages_per_seq=1 << 20)
+    big = dict(max_pages_per_seq=1 << 26)
+    assert call(tokens(((1 << 30) - 3, 0), (3, 1)), **big) == fk.FKV_ENULL and call(tokens(((1 << 30) - 2, 0), (3, 1)), **big) == fk.FKV_EUNSUPPORTED
     assert call(tokens((0, 5), ((1 << 22) - 1, 1)), **big) == fk.FKV_ENULL and call(tokens((0, 5), (1 << 22, 1)), **big) == fk.FKV_EUNSUPPORTED
     assert call(tokens(k_stride=1016)) == fk.FKV_EINVAL and call(tokens(k_stride=1028)) == fk.FKV_EALIGN and call(tokens(k_stride=-1024)) == fk.FKV_EINVAL
     assert call(tokens(q_stride=4088)) == fk.FKV_EINVAL and call(tokens(v_stride=1 << 40)) == fk.FKV_EINVAL
@@ -112,7 +113,9 @@ def test_quant_calls_refuse(lib):
     assert gather(k=None) == fk.FKV_ENULL and gather(idx=None) == fk.FKV_ENULL and gather(v=None) == fk.FKV_ENULL
     assert gather(v=None, v_pages=None, v_scale=None) == fk.FKV_ENULL and gather(b=i32(7, 20)) == fk.FKV_EINVAL
     assert gather(idx=ODD) == fk.FKV_EALIGN and compress(q=ODD) == fk.FKV_EALIGN and compress(v=None) == fk.FKV_ENULL and compress(b=i32(100, 101)) == fk.FKV_EINVAL
-    assert decode(n=None) == fk.FKV_ENULL and decode(n=i32(-1, 0)) == fk.FKV_EINVAL and decode(n=i32(257, 0)) == fk.FKV_EINVAL and decode(out=ODD) == fk.FKV_EALIGN
+    assert decode(n=None) == fk.FKV_ENULL and decode(n=i32(-1, 0)) == fk.FKV_EINVAL and decode(n=i32(257, 0)) == fk.FKV_EINVAL
+    assert decode(n=i32(1 << 30, 0), max_pages_per_seq=1 << 26) == fk.FKV_ENULL and decode(n=i32((1 << 30) + 1, 0), max_pages_per_seq=1 << 26) == fk.FKV_EUNSUPPORTED
+    assert decode(out=ODD) == fk.FKV_EALIGN
     assert lib.fkv_decode_attention_paged_quant(None, ctypes.byref(s), P, None, n, P, None) == fk.FKV_ENULL
 
 
