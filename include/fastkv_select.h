@@ -311,7 +311,8 @@ typedef struct fkv_quant_pages {
  * sequences of a call must not write into the same block.  Gathering: rows of negative indices are not written and do not count
  * towards a scale.  A table entry outside the pool writes nothing, and is clamped into it by the decode call.
  * Decoding: 0 <= n_per_seq[b] <= 2^30, and a sequence without tokens gives zeros (the padding of a batch); any fp32 scales are read, not only powers
- * of two.  Both contractions are accumulated in fp32 from exact products of what the codes stand for. */
+ * of two.  Entries of a call may share pages: the queries of several new tokens of one sequence are so many entries with the same table row,
+ * each with as many tokens as it sees.  Both contractions are accumulated in fp32 from exact products of what the codes stand for. */
 int fkv_append_kv_paged_quant(fkv_ctx *ctx, const fkv_shape *shape, const fkv_rope *rope, const fkv_new_tokens *tokens,
                               const fkv_quant_pages *pages, void *stream);
 int fkv_gather_kv_paged_quant(fkv_ctx *ctx, const fkv_shape *shape, const void *k, const void *v, const int32_t *idx_kv,

@@ -220,7 +220,7 @@ def check_decode(ctx, rng, ns, hq, hkv, page, block, scale=0.0, powers=True, poi
     got = up((codes, scales))
     out = ctx.fkv_decode_attention_paged_quant(shape, dev(q), *got, torch.from_numpy(table).cuda(), ns)
     assert out.dtype == torch.float32
-    o, worst = out.cpu().numpy(), 0.0
+    o = out.cpu().numpy()
     for b, n in enumerate(ns):
         k, v = (paged.dequant(c, s, table[b], n) for c, s in zip(codes, scales))
         want, bound = paged.attend(paged.bf16_to_f64(q[b]), k, v, scale or 128 ** -0.5)
@@ -246,6 +246,20 @@ def test_decode_batches(ctx, seed):
     ns = [int(n) for n in ns]
     print("case: quant decode batch n=%s" % ns, flush=True)
     check_decode(ctx, rng, ns, 32, 8, 16, 16)
+
+
+def test_decode_entries_may_share_pages(ctx):
+    """Several queries of one sequence, each with the tokens that it sees: entries with the same table row; as one by one."""
+    rng = np.random.default_rng(40)
+    table, n_pages = make_table(rng, [900], 32)
+    codes, scales = full_pools(rng, n_pages, 8, 32, 32)
+    pools, q = up((codes, scales)), bits(rng, 5, 32, 128)
+    ns = [896, 897, 1, 899, 900]
+    out = ctx.fkv_decode_attention_paged_quant(fk.make_shape([8] * 5), dev(q), *pools, torch.from_numpy(np.repeat(table, 5, 0)).cuda(), ns)
+    for i, n in enumerate(ns):
+        k, v = (paged.dequant(c, s, table[0], n) for c, s in zip(codes, scales))
+        want, bound = paged.attend(paged.bf16_to_f64(q[i]), k, v, 128 ** -0.5)
+        assert (np.abs(out[i].cpu().numpy() - want) <= bound).all()
 
 
 def test_decode_poison_stays_in_its_head(ctx):
