@@ -255,12 +255,13 @@ int fkv_decode_attention_paged(fkv_ctx *ctx, const fkv_shape *shape, const void 
                                int32_t page_size, int64_t n_pages, const int32_t *n_per_seq, float *out, void *stream);
 
 /* Rotary position embedding (host struct, read during the call only): columns x, y of pair i of a head's row become
- * x cos(phi) - y sin(phi) and y cos(phi) + x sin(phi), phi = position * inv_freq[i].  The angle is reduced exactly (positions are
- * whole numbers), sine and cosine are fp32 values within 2^-22, and a result is rounded once to what it is stored as. */
+ * x cos(phi) - y sin(phi) and y cos(phi) + x sin(phi), phi = position * inv_freq[i].  However far the position, sine
+ * and cosine are fp32 values within 2^-22 (angles are reduced in whole numbers, not in floating point); a result is rounded once
+ * to what it is stored as. */
 typedef struct fkv_rope {
   int32_t rotary_dim;     /* r: the first r columns of a row take part, the others pass unchanged; a multiple of 16, 16 <= r <= d */
   int32_t interleaved;    /* 0: columns i and i + r/2 are pair i; 1: columns 2i and 2i + 1 */
-  const double *inv_freq; /* host [r/2], radians per position, finite */
+  const double *inv_freq; /* host [r/2], radians per position, finite, at most 256 in size (larger ones: FKV_EUNSUPPORTED) */
 } fkv_rope;
 
 /* The new tokens of a call that appends to a paged cache (host struct; n_new_b of sequence b, packed along tokens in that order). */

@@ -174,7 +174,8 @@ def make_shape(lengths, n_q_heads=32, n_kv_heads=8, head_dim=128, window=8, pool
 
 def make_rope(rotary_dim=128, theta=10000.0, interleaved=False, inv_freq=None):
     """Host descriptor of a rotary position embedding: the first rotary_dim columns of a row turn, pair i by position * inv_freq[i]
-    (theta ** (-2 i / rotary_dim) unless given); pairs are columns (i, i + rotary_dim / 2), or (2 i, 2 i + 1) if interleaved."""
+    (theta ** (-2 i / rotary_dim) unless given; at most 256 in size); pairs are columns (i, i + rotary_dim / 2), or (2 i, 2 i + 1) if
+    interleaved."""
     freq = [theta ** (-2.0 * i / rotary_dim) for i in range(rotary_dim // 2)] if inv_freq is None else [float(f) for f in inv_freq]
     if len(freq) != rotary_dim // 2:
         raise ValueError("inv_freq holds %d frequencies, %d columns have %d pairs" % (len(freq), rotary_dim, rotary_dim // 2))

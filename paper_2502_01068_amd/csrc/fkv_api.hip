@@ -1209,6 +1209,9 @@ uint64_t turns_of(double f) {
   return (bits >> 63) != 0 ? 0 - turns : turns;
 }
 
+// Largest frequency, radians per position.  turns_of is off by 2^-65 (f / 2 pi + 1) turns, 2 / pi and the result being rounded; times a position of
+// up to 2^31 that is 41.8 * 2^-34 turns here, 2^-25.9 radians: below the error of the sine and cosine (2^-23).
+constexpr double kRopeMaxFreq = 256.0;
 constexpr int64_t kPagedMaxTokens = 1 << 30;  // of a sequence: a tile's or block's last place stays below 2^31
 constexpr int64_t kAppendMaxTokens = 1 << 22;  // a launch has less than 2^32 threads, at most 640 a token
 
@@ -1235,6 +1238,7 @@ int fill_append(const Resolved &r, const fkv_rope *rope, const fkv_new_tokens *t
     a->interleaved = rope->interleaved;
     for (int i = 0; i < a->pairs; ++i) {
       if (!isfinite(rope->inv_freq[i])) return FKV_EINVAL;
+      if (fabs(rope->inv_freq[i]) > kRopeMaxFreq) return FKV_EUNSUPPORTED;
       a->freq[i] = turns_of(rope->inv_freq[i]);
     }
   } else if (t->q || t->q_out) {

@@ -1,4 +1,6 @@
 """New tokens into a bf16 paged cache, keys and queries turned on the way, against the 64-bit oracle."""
+from fractions import Fraction
+
 import numpy as np
 import pytest
 import torch
@@ -138,3 +140,21 @@ def test_no_new_token_is_no_call(ctx):
     out = ctx.fkv_append_kv_paged(shape, none, none, [3, 16], [0, 0], tab, *pools, rope=fk.make_rope(), positions=torch.empty(0, dtype=torch.int32, device="cuda"),
                                   q=torch.empty((0, 4, 128), dtype=torch.bfloat16, device="cuda"))
     assert out.shape == (0, 4, 128) and all((p == 1).all() for p in pools)
+
+
+def test_the_largest_frequencies_and_positions(ctx):
+    """Angles of up to 2^39 radians.  Rows are (1, 0) per pair, so what is stored is bf16(cos), bf16(sin): off by 2^-22 and one rounding, 2^-8 of the
+    value; the angle itself is reduced here in exact arithmetic."""
+    turn = 2 * Fraction("3.14159265358979323846264338327950288419716939937510582097494459")
+    rng = np.random.default_rng(11)
+    positions = np.concatenate([[2 ** 31 - 1, -2 ** 31, 2 ** 31 - 2, -1, 0, 1], rng.integers(-2 ** 31, 2 ** 31, 122)]).astype(np.int32)
+    freq = np.concatenate([[256.0, -256.0, np.nextafter(256.0, 0), 2.0 ** -60, 1e-300, 0.0, 1 / 3, -1e-7], rng.uniform(-256, 256, 56)])
+    x = np.zeros((128, 1, 128), np.uint16)
+    x[..., :64] = 0x3F80
+    shape, tab = fk.make_shape(8, n_q_heads=1, n_kv_heads=1), torch.arange(2, dtype=torch.int32, device="cuda")[None]
+    pools = [torch.zeros((2, 64, 1, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    ctx.fkv_append_kv_paged(shape, dev(x), dev(x), 0, 128, tab, *pools, rope=fk.make_rope(inv_freq=freq), positions=torch.from_numpy(positions).cuda())
+    angle = np.array([[float((Fraction(int(p)) * Fraction(float(f))) % turn) for f in freq] for p in positions])
+    want = np.concatenate([np.cos(angle), np.sin(angle)], 1)
+    got = paged.bf16_to_f64(host_bits(pools[0])).reshape(128, 128)
+    assert (np.abs(got - want) <= np.abs(want) * 2.0 ** -8 + 2.0 ** -22 * (1 + 2.0 ** -8)).all()

@@ -169,3 +169,10 @@ def test_quant_pages_helper():
         fk.quant_pages(4, 16, scale_block=32)
     k, v, ks, vs = fk.quant_pages(4, 64, n_kv_heads=2, scale_block=32, device="cpu")
     assert k.shape == v.shape == (4, 2, 64, 128) and ks.shape == vs.shape == (4, 2, 2) and k.dtype == torch.float8_e4m3fn and ks.dtype == torch.float32
+
+
+def test_frequencies_that_the_angles_cannot_hold_are_refused(lib):
+    for f, code in ((256.0, fk.FKV_ENULL), (-256.0, fk.FKV_ENULL), (0.0, fk.FKV_ENULL), (5e-324, fk.FKV_ENULL), (256.0 * (1 + 2.0 ** -52), fk.FKV_EUNSUPPORTED),
+                    (-1e6, fk.FKV_EUNSUPPORTED), (2.0 ** 118, fk.FKV_EUNSUPPORTED)):  # ENULL: only the context is missing
+        for quant in (False, True):
+            assert append(lib, tokens(), fk.make_rope(16, inv_freq=[1.0] * 7 + [f]), quant) == code, f
