@@ -299,7 +299,8 @@ int fkv_append_kv_paged(fkv_ctx *ctx, const fkv_shape *shape, const fkv_rope *ro
  * a <= 448 p(a), a = max |x| over the finite x of X.  A block without earlier tokens of the sequence takes the scale s' = p(a) whatever
  * it held; one that earlier tokens lie in takes s' = max(s, p(a)), and where that is larger than its scale s the earlier codes become
  * e4m3(code * s / s') (a power of two: exact, except where a code leaves e4m3's normal range).  X becomes e4m3(x / s'), rounded once, to
- * nearest even; what is not finite becomes NaN.  Powers of two cost no precision, e4m3 being a floating format. */
+ * nearest even; what is not finite becomes NaN.  Powers of two cost no precision, e4m3 being a floating format.  (Behind a scale s that is
+ * not a power of two, which these calls never leave, x / s' and s / s' are rounded to fp32 first.) */
 typedef struct fkv_quant_pages {
   void *k_pages, *v_pages;
   float *k_scale, *v_scale;
