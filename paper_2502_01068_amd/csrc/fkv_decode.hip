@@ -353,16 +353,36 @@ DecodePlan plan_decode(DecodeArgs &a, int n_cu, int waves, bool whole_rounds) {
       share = (share + waves - 1) / waves * waves;
       if (share == waves && 2 * (int64_t)a.tiles > share * n_cu) share *= 2;
     }
-    while (true) {
+    auto cut = [&]() {  // tiles of the longest piece
+      int64_t most = 0;
       a.piece0[0] = 0;
       for (int b = 0; b < a.n_seq; ++b) {
         const int64_t t = a.tile0[b + 1] - a.tile0[b];
         int64_t n = even || t <= whole_tiles ? 1 : std::min<int64_t>((2 * t + share) / (2 * share), kDecodeMaxSplits);
-        a.piece0[b + 1] = a.piece0[b] + (int)std::max<int64_t>(n, 1);
+        n = std::max<int64_t>(n, 1);
+        most = std::max(most, (t + n - 1) / n);
+        a.piece0[b + 1] = a.piece0[b] + (int)n;
       }
-      // nor a second round of few blocks (160 rows of 768 tokens in 320 pieces 16.9, whole 11.2)
-      if (!whole_rounds || a.piece0[a.n_seq] * a.Hkv <= n_cu || a.piece0[a.n_seq] == a.n_seq) break;
-      share += waves;
+      return most;
+    };
+    auto one_round = [&] { return a.piece0[a.n_seq] * a.Hkv <= n_cu || a.piece0[a.n_seq] == a.n_seq; };
+    const int64_t most = cut();
+    // In 8 bits nor a second round of few blocks: longer pieces that fit one round (160 rows of 768 tokens 11.2 us, in 320 pieces 16.8; 56 of 60000
+    // in 224 pieces 135, in 280 196), unless the longest then outweighs what the two rounds come to, two pieces of the mean and a start: beside many short
+    // rows there is no room for pieces of a long one, but the short ones end early (31 sequences of 400 tokens and one of 16000 16.2, in one
+    // round 101; 63 of 500 and one of 60000 42, in one round 481).  Pieces of `share` tiles are less than n_cu + rows: at most kDecodeMaxBlocks.
+    if (whole_rounds && !one_round()) {
+      const int64_t short_share = share, blocks = a.piece0[a.n_seq] * a.Hkv;
+      const int64_t limit = std::max(most, (2 * (int64_t)a.tiles + blocks - 1) / blocks) + waves;
+      bool fits = true;
+      while (fits && !one_round()) {
+        share += std::max<int64_t>(waves, share / 16 / waves * waves);
+        fits = cut() <= limit;
+      }
+      if (!fits) {
+        share = short_share;
+        cut();
+      }
     }
     return {a.piece0[a.n_seq] * a.Hkv, true};
   }

@@ -4,6 +4,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <algorithm>
 #include <map>
 #include <string>
 #include <vector>
@@ -15,6 +16,7 @@ struct Launch {
   std::string kernel;
   unsigned grid[3], block;
   unsigned long long wait_ticks;  // of kernels that wait for other blocks
+  int tiles;                      // of the decode kernels: of the block that has the most
 };
 std::map<const void *, std::string> &kernels() {
   static std::map<const void *, std::string> m;
@@ -38,6 +40,17 @@ const char *recorder_kernel(int i) { return launches[i].kernel.c_str(); }
 unsigned recorder_blocks(int i) { return launches[i].grid[0] * launches[i].grid[1] * launches[i].grid[2]; }
 unsigned recorder_threads(int i) { return launches[i].block; }
 unsigned long long recorder_wait_ticks(int i) { return launches[i].wait_ticks; }
+int recorder_tiles(int i) { return launches[i].tiles; }
+
+static int tiles_of_longest(const fkv::DecodeArgs &a, bool aligned, int blocks) {
+  if (!aligned) return (a.tiles + blocks - 1) / blocks;
+  int most = 0;
+  for (int b = 0; b < a.n_seq; ++b) {
+    const int n = a.piece0[b + 1] - a.piece0[b];
+    most = std::max(most, (a.tile0[b + 1] - a.tile0[b] + n - 1) / n);
+  }
+  return most;
+}
 
 void **__hipRegisterFatBinary(const void *) {
   static void *handle;
@@ -78,10 +91,12 @@ hipError_t hipLaunchKernel(const void *f, dim3 grid, dim3 block, void **args, si
     fail_at = -1;
     return last_error = hipErrorLaunchFailure;
   }
-  Launch l{kernels()[f], {grid.x, grid.y, grid.z}, block.x * block.y * block.z, 0};
+  Launch l{kernels()[f], {grid.x, grid.y, grid.z}, block.x * block.y * block.z, 0, 0};
   auto has = [&](const char *name) { return l.kernel.find(name) != std::string::npos; };
   if (has("k_wout_partial")) l.wait_ticks = static_cast<const fkv::WoutArgs *>(args[0])->timeout_ticks;
   if (has("k_score_fused") || has("k_score_keep")) l.wait_ticks = static_cast<const fkv::FusedArgs *>(args[1])->timeout_ticks;
+  if (has("k_decode_quant<")) l.tiles = tiles_of_longest(static_cast<const fkv::DecodeQuantArgs *>(args[0])->d, has("<true"), (int)grid.x);
+  if (has("k_decode<")) l.tiles = tiles_of_longest(*static_cast<const fkv::DecodeArgs *>(args[0]), has("<true, true") || has("<false, true"), (int)grid.x);
   launches.push_back(l);
   return hipSuccess;
 }

@@ -2,7 +2,8 @@
 hip_recorder.cpp stands in for the HIP runtime (256 compute units, one block of a resident kernel on each); nothing runs.
 
 A step is a list: an operation and its keywords.  What comes back for each step is its status and its launches
-(kernel, blocks, threads, wait limit in 100 MHz ticks of those that wait for other blocks), or the value asked for."""
+(kernel, blocks, threads, wait limit in 100 MHz ticks of those that wait for other blocks, tiles of 32 tokens of the decode kernels' longest
+block), or the value asked for."""
 import ctypes
 import json
 import os
@@ -36,6 +37,11 @@ class _Shape(ctypes.Structure):
     _fields_ = [("n_seq", ctypes.c_int32), ("cu_seqlens", ctypes.POINTER(ctypes.c_int32))] + [
         (n, ctypes.c_int32) for n in ("L", "n_q_heads", "n_kv_heads", "head_dim", "window", "pool_kernel", "pool_mode")] + [
         ("softmax_scale", ctypes.c_float), ("causal", ctypes.c_int32)]
+
+
+class _QuantPages(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_pages", "v_pages", "k_scale", "v_scale", "block_table")] + [
+        (n, ctypes.c_int32) for n in ("max_pages_per_seq", "page_size", "scale_block")] + [("n_pages", ctypes.c_int64)]
 
 
 def _i32(values):
@@ -106,6 +112,15 @@ class _Calls:
         return self.lib.fkv_compress_kv(self.ctx[0], s, p, p, p, _i32(budgets), p, p, p, p if tsp else None, ctypes.c_size_t(2 * hidden),
                                         _i32(k_tsp) if tsp else None, p if tsp else None, p if tsp else None, None)
 
+    def decode(self, n, quant=True, page=16, hq=32, hkv=8):
+        """Over pages, in 8 bits or bf16; one page more than the longest sequence fills."""
+        s, _keep = self._shape([8] * len(n), hq=hq, hkv=hkv)
+        p, counts, most = self.ptr, _i32(n), max(n) // page + 1
+        if not quant:
+            return self.lib.fkv_decode_attention_paged(self.ctx[0], s, p, p, p, p, most, page, ctypes.c_int64(1000), counts, p, None)
+        pages = _QuantPages(*[1 << 20] * 5, most, page, 16, 1000)
+        return self.lib.fkv_decode_attention_paged_quant(self.ctx[0], s, p, ctypes.byref(pages), counts, p, None)
+
 
 def _main():
     rec = ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL)  # ahead of the library, whose runtime calls find it first
@@ -119,7 +134,7 @@ def _main():
         value = getattr(calls, op)(**kw)
         results.append({"value": value, "launches": [
             {"kernel": rec.recorder_kernel(i).decode(), "blocks": rec.recorder_blocks(i), "threads": rec.recorder_threads(i),
-             "wait_ticks": rec.recorder_wait_ticks(i)} for i in range(rec.recorder_launches())]})
+             "wait_ticks": rec.recorder_wait_ticks(i), "tiles": rec.recorder_tiles(i)} for i in range(rec.recorder_launches())]})
     json.dump(results, sys.stdout)
 
 

@@ -1,0 +1,54 @@
+"""Decode over a cache in 8 bits in each of the ways its rows are spread over the blocks: which way a case takes is looked at by
+test_paged_launches_host.py, without a GPU."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged
+from paper_2502_01068_amd import binding as fk
+from test_gpu_append import bits, dev, make_table
+from test_gpu_quant import full_pools, up
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = fk.Context(max_total_tokens=4096, max_seqs=64)
+    yield c
+    c.close()
+
+
+# tokens of the entries, heads, page, scale block, the kernel <rows cut apart, waves>, tiles of its longest block
+UNEVEN = [
+    ([400] * 15 + [16000] + [400] * 16, 32, 8, 16, 16, "<true, 8>", 32), ([0] * 11 + [300] * 20 + [9001], 8, 8, 64, 32, "<true, 8>", 16),
+    ([500] * 40 + [20000] + [500] * 23, 32, 8, 16, 16, "<true, 4>", 29), ([7000, 0] + [515, 33] * 30, 16, 8, 32, 32, "<true, 4>", 17),
+]
+
+
+def check(ctx, ns, hq, hkv, page, block, distinct=None):
+    """Entry b attends over the first ns[b] tokens of sequence b % distinct (its own one unless given).  Checked: the first entries, the last, the longest
+    and shortest, each against 64 bits."""
+    B, rng = len(ns), np.random.default_rng(sum(ns) + hq + page)
+    lengths = [max(ns[b::distinct]) for b in range(distinct)] if distinct else ns
+    table, n_pages = make_table(rng, lengths, page)
+    table = table[np.arange(B) % len(lengths)]
+    codes, scales = full_pools(rng, n_pages, hkv, page, block, powers=False)
+    q = bits(rng, B, hq, 128)
+    shape = fk.make_shape([8] * B, n_q_heads=hq, n_kv_heads=hkv)
+    args = (shape, dev(q), *up((codes, scales)), torch.from_numpy(table).cuda(), ns)
+    out = ctx.fkv_decode_attention_paged_quant(*args)
+    assert torch.equal(out, ctx.fkv_decode_attention_paged_quant(*args))
+    o = out.cpu().numpy()
+    assert np.isfinite(o).all() and not o[np.array(ns) == 0].any()
+    off = lambda b, row: np.abs(o[b] - (ref := paged.attend(paged.bf16_to_f64(q[b]), *(paged.dequant(c, s, row, ns[b]) for c, s in zip(codes, scales)),
+                                                            128 ** -0.5))[0]) - ref[1]
+    for b in sorted({0, 1, B - 1, int(np.argmax(ns)), int(np.argmin(ns))}):
+        assert (off(b, table[b]) <= 0).all(), (b, ns[b])
+    return off, table
+
+
+@pytest.mark.parametrize("ns,hq,hkv,page,block,kernel,tiles", UNEVEN)
+def test_a_long_sequence_among_short_ones(ctx, ns, hq, hkv, page, block, kernel, tiles):
+    print("case: quant decode uneven %d x %d, heads=%d/%d page=%d block=%d" % (len(ns), max(ns), hq, hkv, page, block), flush=True)
+    check(ctx, ns, hq, hkv, page, block)
