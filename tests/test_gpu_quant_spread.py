@@ -24,6 +24,17 @@ UNEVEN = [
     ([400] * 15 + [16000] + [400] * 16, 32, 8, 16, 16, "<true, 8>", 32), ([0] * 11 + [300] * 20 + [9001], 8, 8, 64, 32, "<true, 8>", 16),
     ([500] * 40 + [20000] + [500] * 23, 32, 8, 16, 16, "<true, 4>", 29), ([7000, 0] + [515, 33] * 30, 16, 8, 32, 32, "<true, 4>", 17),
 ]
+# rows of equal length that are not cut, entries of the same few sequences: a wave asks for its page entries three times, 32 tiles at a time
+REFILL = [
+    ([20000 - 3 * i for i in range(32)], 8, 8, 16, 16, "<true, 8>", 625), ([9000 - i for i in range(64)], 8, 8, 16, 16, "<true, 4>", 282),
+    ([17000 - i for i in range(32)], 16, 8, 64, 64, "<true, 8>", 532),
+]
+# equal shares of the line of all tiles: blocks that go through several rows, rows that several blocks share, empty ones among them
+SHARES = [
+    ([4000 - 7 * i for i in range(20)], 32, 8, 16, 16, "<false, 8>", 78), ([60000] * 3 + [100, 0, 33] * 5 + [0, 1], 8, 4, 64, 32, "<false, 8>", 89),
+    ([0, 2500, 50, 9000] * 12, 32, 8, 16, 16, "<false, 4>", 69), ([3000 - i for i in range(40)], 16, 8, 128, 64, "<false, 4>", 59),
+    ([14000 - i for i in range(20)] + [0, 1], 8, 8, 16, 16, "<false, 8>", 274), ([0] + [12000 - i for i in range(40)], 8, 8, 32, 16, "<false, 4>", 235),
+]
 
 
 def check(ctx, ns, hq, hkv, page, block, distinct=None):
@@ -52,3 +63,21 @@ def check(ctx, ns, hq, hkv, page, block, distinct=None):
 def test_a_long_sequence_among_short_ones(ctx, ns, hq, hkv, page, block, kernel, tiles):
     print("case: quant decode uneven %d x %d, heads=%d/%d page=%d block=%d" % (len(ns), max(ns), hq, hkv, page, block), flush=True)
     check(ctx, ns, hq, hkv, page, block)
+
+
+@pytest.mark.parametrize("ns,hq,hkv,page,block,kernel,tiles", REFILL)
+def test_many_tiles_of_a_wave(ctx, ns, hq, hkv, page, block, kernel, tiles):
+    """A page read in place of another, in tiles behind a wave's first 32 or 64, would be seen: the oracle's result with it is out of bounds."""
+    print("case: quant decode long rows %d x %d, heads=%d/%d page=%d block=%d" % (len(ns), max(ns), hq, hkv, page, block), flush=True)
+    off, table = check(ctx, ns, hq, hkv, page, block, distinct=3)
+    waves = int(kernel[-2])
+    for first in (32, 64):  # tokens of the wave's tile with that number
+        wrong, at = table[0].copy(), first * waves * 32 // page
+        wrong[at] = wrong[at + 1]
+        assert at + 1 < ns[0] // page and (off(0, wrong) > 0).any(), first
+
+
+@pytest.mark.parametrize("ns,hq,hkv,page,block,kernel,tiles", SHARES)
+def test_equal_shares(ctx, ns, hq, hkv, page, block, kernel, tiles):
+    print("case: quant decode equal shares %d x %d, heads=%d/%d page=%d block=%d" % (len(ns), max(ns), hq, hkv, page, block), flush=True)
+    check(ctx, ns, hq, hkv, page, block, distinct=2)

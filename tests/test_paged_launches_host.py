@@ -55,7 +55,7 @@ def test_pieces_fit_the_workspace(calls):
         assert 64 * r["launches"][0]["tiles"] >= _tiles(max(n)), n
 
 
-@pytest.mark.parametrize("case", test_gpu_quant_spread.UNEVEN, ids=lambda c: "%dx%d" % (len(c[0]), max(c[0])))
+@pytest.mark.parametrize("case", test_gpu_quant_spread.UNEVEN + test_gpu_quant_spread.REFILL + test_gpu_quant_spread.SHARES, ids=lambda c: "%dx%d" % (len(c[0]), max(c[0])))
 def test_cases_take_their_kernel(calls, case):
     ns, hq, hkv, page, _, kernel, tiles = case
     launch = calls(("decode", {"n": ns, "hq": hq, "hkv": hkv, "page": page}))[0]["launches"][0]
