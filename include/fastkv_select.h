@@ -311,7 +311,8 @@ typedef struct fkv_quant_pages {
 
 /* fkv_append_kv_paged, fkv_gather_kv_paged, fkv_compress_kv_paged and fkv_decode_attention_paged on such a cache.  Appending: the
  * sequences of a call must not write into the same block.  Gathering: rows of negative indices are not written and do not count
- * towards a scale.  A table entry outside the pool writes nothing, and is clamped into it by the decode call.
+ * towards a scale; they are tokens of the cache all the same, and a head's block of no others takes the smallest scale, 2^-126, for
+ * what is appended behind.  A table entry outside the pool writes nothing, and is clamped into it by the decode call.
  * Decoding: 0 <= n_per_seq[b] <= 2^30, and a sequence without tokens gives zeros (the padding of a batch); any fp32 scales are read, not only powers
  * of two.  Entries of a call may share pages: the queries of several new tokens of one sequence are so many entries with the same table row,
  * each with as many tokens as it sees.  Both contractions are accumulated in fp32 from exact products of what the codes stand for. */

@@ -81,7 +81,8 @@ def append_quant(codes, scales, rows, start, block_table, valid=None):
         first, last = max(tok0, start), min(tok0 + block, start + n)
         for h in range(n_heads):
             put = [t for t in range(first, last) if valid[t - start, h]]
-            if not put:
+            if not put:  # no row is there: the smallest scale, for what is appended behind
+                scales[page, h, slot // block] = SCALE_MIN
                 continue
             x = rows[np.array(put) - start, h]
             at = np.array(put) - tok0 + slot

@@ -212,20 +212,18 @@ __global__ __launch_bounds__(kAppendMaxThreads) void k_append(AppendArgs) {
 
 // One scale block of one head, a wave's work: of its rows 0 .. kBlock - 1 (of kHeadDim bytes at `codes`) those of is_new are new, and
 // earlier tokens lie in the `kept` rows at its begin.  A thread has row p * kRowLanes + lane / kRowLanes of step p, of which value(p, x) gives the
-// 16 numbers of its two chunks.  No new row: nothing is written.
+// 16 numbers of its two chunks.  No new row (a gather of negative indices): the smallest scale, so that none that memory held outlives it.
 template <int kBlock, typename Value>
 __device__ __forceinline__ void store_block(int kept, const bool (&is_new)[kBlock / kRowLanes], uint8_t *codes, float *scale, Value value, RowPart part) {
   constexpr int kSteps = kBlock / kRowLanes;
   const int lane = threadIdx.x & 63, sub = lane / kRowLanes;
   const float old = kept > 0 ? *scale : 0.f;
   float amax = 0.f;
-  bool any = false;
   // The numbers are kept, in 64 registers at most, or formed again: 32 requests 6.2 against 6.6 us, keys and values of 11000 tokens 17.7 against 20.
   constexpr bool kKeep = kBlock <= 32;
   float x[kKeep ? kSteps : 1][16];
 #pragma unroll
   for (int p = 0; p < kSteps; ++p) {
-    any |= is_new[p];
     if (is_new[p]) {
       float (&y)[16] = x[kKeep ? p : 0];
       value(p, y);
@@ -233,7 +231,6 @@ __device__ __forceinline__ void store_block(int kept, const bool (&is_new)[kBloc
       for (int e = 0; e < 16; ++e) amax = fmaxf(amax, is_finite(y[e]) ? __builtin_fabsf(y[e]) : 0.f);
     }
   }
-  if (__builtin_amdgcn_ballot_w64(any) == 0ull) return;
   amax = wave_fmax(amax);
   const float now = fmaxf(scale_for(amax), old), inv = 1.f / now;
   if (kept > 0 && now > old) {

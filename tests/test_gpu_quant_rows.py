@@ -1,5 +1,5 @@
-"""What the calls that fill a cache in 8 bits store: keys turned in every form of the embedding, K gathered alone.
-Against the 64-bit oracle."""
+"""What the calls that fill a cache in 8 bits store: keys turned in every form of the embedding, K gathered alone, blocks that a gather puts
+nothing into.  Against the 64-bit oracle."""
 import numpy as np
 import pytest
 import torch
@@ -85,3 +85,36 @@ def test_keys_gathered_alone(ctx, lengths, budget, hkv, page, block):
     assert res[1] is None and res[3] is None
     gather64(codes, scales, k, idx, lengths, budget, table)
     same(pools, [codes], [scales])
+
+
+@pytest.mark.parametrize("page,block", [(16, 16), (64, 32), (64, 64)])
+def test_appending_behind_rows_that_are_not_there(ctx, page, block):
+    """A head's block of nothing but negative indices counts as filled, so what is appended behind must not meet the scale that memory held."""
+    print("case: quant gather of no rows, append behind, page=%d block=%d" % (page, block), flush=True)
+    rng = np.random.default_rng(page + block)
+    lengths, budget, hkv = [200, 100], [2 * block + 5, 9], 4
+    shape = fk.make_shape(lengths, n_q_heads=hkv, n_kv_heads=hkv)
+    k, v = bits(rng, 300, hkv, 128), bits(rng, 300, hkv, 128)
+    table, n_pages = make_table(rng, [b + 8 for b in budget], page)
+    codes, _ = noise_pools(rng, n_pages, hkv, page, block)
+    scales = [np.full((n_pages, hkv, page // block), 1e30, np.float32) for _ in range(2)]
+    got, tab = up((codes, scales)), torch.from_numpy(table).cuda()
+    idx = np.concatenate([np.stack([np.sort(rng.choice(n, b, replace=False)) for _ in range(hkv)]) for n, b in zip(lengths, budget)], 1).astype(np.int32)
+    idx[1] = -1                               # all of a head
+    idx[2, block:sum(budget)] = -1            # of the first sequence all but its first block, the second sequence
+    ctx.fkv_gather_kv_paged_quant(shape, dev(k), dev(v), torch.from_numpy(idx).cuda(), budget, tab, *got)
+    for i, x in enumerate((k, v)):
+        gather64(codes[i], scales[i], x, idx, lengths, budget, table)
+    assert scales[0][table[0][0], 1, 0] == 2.0 ** -126
+    same(got, codes, scales)
+    new = bits(rng, 9, 2 * hkv, 128)
+    ctx.fkv_append_kv_paged_quant(shape, dev(new)[:, :hkv], dev(new)[:, hkv:], budget, [8, 1], tab, *got)
+    x = paged.bf16_to_f64(new)
+    for i, rows in enumerate((x[:, :hkv], x[:, hkv:])):
+        paged.append_quant(codes[i], scales[i], rows[:8], budget[0], table[0])
+        paged.append_quant(codes[i], scales[i], rows[8:], budget[1], table[1])
+    same(got, codes, scales)
+    for at, row in ((budget[0], 0), (budget[1], 8)):  # the tokens are there, within half a step of a scale that is theirs
+        p, s = table[0 if row < 8 else 1][at // page], at % page
+        v64 = paged.e4m3_decode(got[0].cpu().numpy()[p, :, s]) * got[2].cpu().numpy()[p, :, s // block][:, None].astype(np.float64)
+        assert (np.abs(v64 - x[row, :hkv]) <= np.abs(x[row, :hkv]) * 2.0 ** -4 + got[2].cpu().numpy()[p, :, s // block][:, None] * 2.0 ** -10).all()
