@@ -1196,22 +1196,24 @@ int check_stride(int64_t given, int heads, int64_t *out) {
   return *out % 8 != 0 ? FKV_EALIGN : FKV_OK;
 }
 
-// f / (2 pi) without its whole turns, in units of 2^-64.  f is mant * 2^(exp - 1075), and 2 / pi = 0xA2F9836E4E44152A * 2^-64 but for
-// 2^-65: the product of the two whole numbers, shifted.  (In 80-bit floating point a frequency took 0.2 us.)
-uint64_t turns_of(double f) {
-  uint64_t bits;
-  memcpy(&bits, &f, sizeof bits);
-  const int exp = (int)(bits >> 52) & 0x7FF, shift = 1077 - exp;  // to the right: 1075 - exp + 66 - 64
-  if (exp == 0 || shift > 117) return 0;
-  const uint64_t mant = (bits & (((uint64_t)1 << 52) - 1)) | (uint64_t)1 << 52;
-  const unsigned __int128 p = (unsigned __int128)mant * 0xA2F9836E4E44152Aull;
-  const uint64_t turns = shift > 0 ? (uint64_t)(((p >> (shift - 1)) + 1) >> 1) : shift > -64 ? (uint64_t)p << -shift : 0;
-  return (bits >> 63) != 0 ? 0 - turns : turns;
-}
-
 // Largest frequency, radians per position.  turns_of is off by 2^-65 (f / 2 pi + 1) turns, 2 / pi and the result being rounded; times a position of
 // up to 2^31 that is 41.8 * 2^-34 turns here, 2^-25.9 radians: below the error of the sine and cosine (2^-23).
 constexpr double kRopeMaxFreq = 256.0;
+
+// f / (2 pi) without its whole turns, in units of 2^-64, for |f| <= kRopeMaxFreq.  f is mant * 2^(exp - 1075), and 2 / pi = 0xA2F9836E4E44152A * 2^-64
+// but for 2^-65: the product of the two whole numbers (below 2^117), shifted to the right by 46 or more.  (In 80-bit floating point a frequency
+// took 0.2 us.)
+uint64_t turns_of(double f) {
+  uint64_t bits;
+  memcpy(&bits, &f, sizeof bits);
+  const int exp = (int)(bits >> 52) & 0x7FF, shift = 1077 - exp;  // 1075 - exp + 66 - 64
+  if (exp == 0 || shift > 117) return 0;
+  const uint64_t mant = (bits & (((uint64_t)1 << 52) - 1)) | (uint64_t)1 << 52;
+  const unsigned __int128 p = (unsigned __int128)mant * 0xA2F9836E4E44152Aull;
+  const uint64_t turns = (uint64_t)(((p >> (shift - 1)) + 1) >> 1);
+  return (bits >> 63) != 0 ? 0 - turns : turns;
+}
+
 constexpr int64_t kPagedMaxTokens = 1 << 30;  // of a sequence: a tile's or block's last place stays below 2^31
 constexpr int64_t kAppendMaxTokens = 1 << 22;  // a launch has less than 2^32 threads, at most 640 a token
 
