@@ -300,7 +300,7 @@ int fkv_append_kv_paged(fkv_ctx *ctx, const fkv_shape *shape, const fkv_rope *ro
  * it held; one that earlier tokens lie in takes s' = max(s, p(a)), and where that is larger than its scale s the earlier codes become
  * e4m3(code * s / s') (a power of two: exact, except where a code leaves e4m3's normal range).  X becomes e4m3(x / s'), rounded once, to
  * nearest even; what is not finite becomes NaN.  Powers of two cost no precision, e4m3 being a floating format.  (Behind a scale s that is
- * not a power of two, which these calls never leave, x / s' and s / s' are rounded to fp32 first.) */
+ * not a power of two, which these calls never leave, x / s' and s / s' are rounded to fp32 first; s has to be positive and finite.) */
 typedef struct fkv_quant_pages {
   void *k_pages, *v_pages;
   float *k_scale, *v_scale;
@@ -313,9 +313,11 @@ typedef struct fkv_quant_pages {
  * sequences of a call must not write into the same block.  Gathering: rows of negative indices are not written and do not count
  * towards a scale; they are tokens of the cache all the same, and a head's block of no others takes the smallest scale, 2^-126, for
  * what is appended behind.  A table entry outside the pool writes nothing, and is clamped into it by the decode call.
- * Decoding: 0 <= n_per_seq[b] <= 2^30, and a sequence without tokens gives zeros (the padding of a batch); any fp32 scales are read, not only powers
- * of two.  Entries of a call may share pages: the queries of several new tokens of one sequence are so many entries with the same table row,
- * each with as many tokens as it sees.  Both contractions are accumulated in fp32 from exact products of what the codes stand for. */
+ * Decoding: 0 <= n_per_seq[b] <= 2^30, and a sequence without tokens gives zeros (the padding of a batch).  Scales of either sign are read,
+ * not only powers of two: K's as long as logits stay finite, V's from 2^-80 to 2^80 in size (a token's product loses what lies below
+ * 2^-126, sums of larger ones may overflow before they are divided); a non-finite one makes NaN of what its block's tokens enter.
+ * Entries of a call may share pages: the queries of several new tokens of one sequence are so many entries with the same table row, each
+ * with as many tokens as it sees.  Both contractions are accumulated in fp32 from exact products of what the codes stand for. */
 int fkv_append_kv_paged_quant(fkv_ctx *ctx, const fkv_shape *shape, const fkv_rope *rope, const fkv_new_tokens *tokens,
                               const fkv_quant_pages *pages, void *stream);
 int fkv_gather_kv_paged_quant(fkv_ctx *ctx, const fkv_shape *shape, const void *k, const void *v, const int32_t *idx_kv,

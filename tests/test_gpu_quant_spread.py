@@ -81,3 +81,35 @@ def test_many_tiles_of_a_wave(ctx, ns, hq, hkv, page, block, kernel, tiles):
 def test_equal_shares(ctx, ns, hq, hkv, page, block, kernel, tiles):
     print("case: quant decode equal shares %d x %d, heads=%d/%d page=%d block=%d" % (len(ns), max(ns), hq, hkv, page, block), flush=True)
     check(ctx, ns, hq, hkv, page, block, distinct=2)
+
+
+@pytest.mark.parametrize("k_exp,v_exp", [(-8, -80), (-8, 79), (-126, 0), (-4, 0)])
+def test_scales_at_the_edges(ctx, k_exp, v_exp):
+    """Scales of either sign, not powers of two, as small and as large as they may be: within the bound of fp32 sums."""
+    print("case: quant decode, scales about 2^%d (K), 2^%d (V)" % (k_exp, v_exp), flush=True)
+    rng, ns = np.random.default_rng(abs(v_exp - k_exp)), [700, 40]
+    table, n_pages = make_table(rng, ns, 16)
+    codes, scales = full_pools(rng, n_pages, 8, 16, 16)
+    scales = [(np.ldexp(rng.uniform(1, 2, s.shape), e) * rng.choice([-1, 1], s.shape)).astype(np.float32) for s, e in zip(scales, (k_exp, v_exp))]
+    q = bits(rng, 2, 32, 128)
+    out = ctx.fkv_decode_attention_paged_quant(fk.make_shape([8, 8]), dev(q), *up((codes, scales)), torch.from_numpy(table).cuda(), ns).cpu().numpy()
+    for b, n in enumerate(ns):
+        want, bound = paged.attend(paged.bf16_to_f64(q[b]), *(paged.dequant(c, s, table[b], n) for c, s in zip(codes, scales)), 128 ** -0.5)
+        assert (np.abs(out[b] - want) <= bound).all(), (b, (np.abs(out[b] - want) / bound).max())
+
+
+@pytest.mark.parametrize("which", [0, 1])
+@pytest.mark.parametrize("value", [np.nan, np.inf])
+def test_scales_that_are_not_finite(ctx, which, value):
+    """NaN in the outputs of the block's head, and nowhere else."""
+    rng, ns = np.random.default_rng(50), [70, 300]
+    shape = fk.make_shape([8, 8], n_q_heads=8, n_kv_heads=4)
+    table, n_pages = make_table(rng, ns, 16)
+    codes, scales = full_pools(rng, n_pages, 4, 16, 16)
+    q, tab = dev(bits(rng, 2, 8, 128)), torch.from_numpy(table).cuda()
+    clean = ctx.fkv_decode_attention_paged_quant(shape, q, *up((codes, scales)), tab, ns)
+    scales[which][table[1][18], 3, 0] = value  # tokens 288 .. 299 of sequence 1, head 3
+    out = ctx.fkv_decode_attention_paged_quant(shape, q, *up((codes, scales)), tab, ns)
+    bad = torch.zeros_like(out, dtype=torch.bool)
+    bad[1, 6:8] = True
+    assert torch.equal(out.isnan(), bad) and torch.equal(out[~bad], clean[~bad])
