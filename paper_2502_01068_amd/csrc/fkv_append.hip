@@ -30,7 +30,7 @@ struct TurnTable {
 
 // Sine and cosine of 2 pi t / 2^32.  The two top bits, rounded, are the quarter; what is left, a at most pi/4 in size, goes into Taylor's
 // series, cut off where the next term is below 2^-28 (a^11 / 11!) and 2^-30 (a^12 / 12!).  Within 2^-23 in all.  Shorter than the library's
-// sincospif: 64 tokens 4.6 -> 4.2 us.
+// sincospif: 64 tokens 4.6 -> 4.3 us.
 __device__ __forceinline__ void turn_sincos(uint32_t t, float *sn, float *cs) {
   const uint32_t quarter = (t + 0x20000000u) >> 30;
   const float a = (float)(int32_t)(t - (quarter << 30)) * 1.46291807926715968e-9f;  // 2 pi / 2^32
